@@ -45,8 +45,10 @@ enum {
   BASS_STATUS_LEN_CLAMPED = 1,      /* a ctx_len / draft_len / n_new / n_draft was out of range */
   BASS_STATUS_TOKEN_CLAMPED = 2,    /* a draft token id was outside [0, V)                      */
   BASS_STATUS_ZERO_MASS = 4,        /* a probability row had no mass to sample from             */
-  BASS_STATUS_PLAN_MISMATCH = 8     /* the plan handed to an attention launch was made for another
+  BASS_STATUS_PLAN_MISMATCH = 8,    /* the plan handed to an attention launch was made for another
                                        shape, work spread or kind of launch; nothing was computed */
+  BASS_STATUS_PAGE_CLAMPED = 16,    /* a page number or slot that was needed was outside the pool       */
+  BASS_STATUS_NO_PAGES = 32         /* bass_page_tables: too few free pages for some rows               */
 };
 
 /* BASS_DTYPE_INT8KV: Q, K_new, V_new are bf16; the caches hold INT8 codes with one fp32 scale per
@@ -300,6 +302,106 @@ int bass_warp_accept(int32_t B, int32_t kmax, int32_t V, const float* logits_mai
                      const int32_t* draft_tok, const int32_t* n_draft, const float* u,
                      int32_t* n_accept, int32_t* next_token, int32_t* ctx_len, void* workspace,
                      size_t workspace_bytes, int32_t* dev_status, void* stream);
+
+/*
+ * Paged caches.  Several answers to one prompt, or many requests behind one system prompt, hold the same first
+ * tokens: the paper's batches are of this kind (several sequences sampled from one prompt).  Their keys and values are kept once, in
+ * pages that the sequences' tables share, and bass_paged_verify_attention reads them once for all.
+ *
+ * A pool is [n_pages][Hkv][page_tokens / 32] blocks of 32 tokens, one pool for K and one for V.  Token t of sequence b lies in page
+ * tables[b][t / page_tokens], at t % page_tokens; its slot is page * page_tokens + t % page_tokens.  A block holds, in the order of
+ * [token of the block][head element d],
+ *   bf16, 32 D elements:                  K [token / 16][d / 32][d / 8 % 4][token % 16][d % 8]
+ *                                         V [d / 16][token / 4 % 4][d % 16][token / 16][token % 4]
+ *   INT8, 32 D codes, then 32 fp32 scales: K [token / 16][d / 64][d / 16 % 4][token % 16][d % 16]
+ *                                         V [d / 32][token / 4 % 4][d % 16][d / 16 % 2][token / 16][token % 4]
+ * (operand order of the matrix instructions, as in the caches above; codes and scales are those of BASS_DTYPE_INT8KV).  A pool is 16-byte aligned.
+ * Every layer has pools of its own; the tables serve all layers.
+ */
+typedef struct bass_paged_desc {
+  int32_t B;           /* sequences in the batch, at most 4096                                              */
+  int32_t kmax;        /* query-token slots per sequence                                                    */
+  int32_t Hq, Hkv, D;  /* as in bass_attn_desc; D: 64 or 128                                                 */
+  int32_t page_tokens; /* tokens of a page: a multiple of 32                                                 */
+  int32_t n_pages;     /* pages of a pool; n_pages * page_tokens < 2^31                                      */
+  int32_t max_pages;   /* entries of a sequence's table                                                      */
+  int32_t dtype;       /* BASS_DTYPE_BF16 or BASS_DTYPE_INT8KV: the pools; Q, K_new, V_new and O are bf16     */
+  float scale;
+} bass_paged_desc;
+
+/* Bytes of ONE pool (K or V); 0 for a bad shape. */
+size_t bass_page_pool_bytes(const bass_paged_desc* desc);
+
+/*
+ * Tables and slots from the rows' lengths: pages are taken, shared and given back on the GPU.  A row is a sequence, or anything else
+ * that holds pages (a prompt that requests begin with); all arrays are on the device.
+ *   length     [rows]             tokens each row has to have room for; 0 = it gives all its pages back
+ *   share_from [rows] or NULL     a row without pages begins with the first pages of row share_from (negative: of none) ...
+ *   share_len  [rows] or NULL     ... as many whole pages as share_len tokens fill, at most what that row holds at the call's start
+ *   held       [rows] in/out      pages of each row (0 before its first call)
+ *   tables     [rows, max_pages] in/out   page numbers; entries from held on are written as -1 where the call gives pages back
+ *   refs       [n_pages] in/out   rows that hold each page (all 0 before the first call); 0 = the page is free
+ *   ctx_len, n_new [rows], slots [rows, kmax] out: optional (slots NULL: none); slot of token ctx_len + i for i < n_new that has a
+ *              place in the row's pages, -1 for the others
+ * In this order: rows share; rows that hold more pages than ceil(length / page_tokens) give the last ones back (a page is free
+ * when no row holds it); rows that hold fewer take free pages, the lowest numbers first, row after row.  The first row that finds too few,
+ * and all rows behind it that need any, take none (BASS_STATUS_NO_PAGES): their tables stay valid for what they hold.
+ * Lengths below 0 or over max_pages * page_tokens are clamped, n_new to [0, kmax] (BASS_STATUS_LEN_CLAMPED); a share_from that is no row or the
+ * row itself shares nothing (BASS_STATUS_LEN_CLAMPED).  Entries that are no page are neither shared nor counted (BASS_STATUS_PAGE_CLAMPED).
+ * The result does not depend on the order in which anything runs.  rows, max_pages, n_pages > 0, page_tokens a multiple of 32, rows * max_pages < 2^31,
+ * n_pages * page_tokens < 2^31, 0 <= kmax <= 65535.  workspace: device, 16-byte aligned, at least bass_page_tables_workspace_bytes(rows, n_pages) bytes,
+ * contents irrelevant on entry.  Three launches.
+ */
+size_t bass_page_tables_workspace_bytes(int32_t rows, int32_t n_pages);
+int bass_page_tables(int32_t rows, int32_t max_pages, int32_t page_tokens, int32_t n_pages, const int32_t* length,
+                     const int32_t* share_from, const int32_t* share_len, int32_t* held, int32_t* tables, int32_t* refs, int32_t kmax,
+                     const int32_t* ctx_len, const int32_t* n_new, int32_t* slots, void* workspace, size_t workspace_bytes,
+                     int32_t* dev_status, void* stream);
+
+/*
+ * Keys and values of new tokens into the pages: row i of sequence b, K_new, V_new [B, kmax, Hkv, D] bf16, to slot slots[b, i]
+ * (slots [B, kmax] int32; negative: the row is left out; beyond the pool: left out, BASS_STATUS_PAGE_CLAMPED).  INT8 pools: quantized as in
+ * bass_kv_append.  Nothing but the rows' own bytes is written.  Two rows of one call must not have the same slot.
+ */
+int bass_paged_append(const bass_paged_desc* desc, void* Kpool, void* Vpool, const void* K_new, const void* V_new,
+                      const int32_t* slots, int32_t* dev_status, void* stream);
+
+/*
+ * Tokens start[b] .. start[b] + n[b] - 1 of every sequence read back through its table [B, max_pages] into K_out, V_out [B, kmax, Hkv, D]
+ * (bf16 pools); other rows are left untouched, and so are those of tokens beyond the table (BASS_STATUS_LEN_CLAMPED) or without a page
+ * (BASS_STATUS_PAGE_CLAMPED).  _int8: codes and scales of INT8 pools, as in bass_kv_gather_int8.
+ */
+int bass_paged_gather(const bass_paged_desc* desc, const void* Kpool, const void* Vpool, void* K_out, void* V_out,
+                      const int32_t* tables, const int32_t* start, const int32_t* n, int32_t* dev_status, void* stream);
+int bass_paged_gather_int8(const bass_paged_desc* desc, const void* Kpool, const void* Vpool, int8_t* K_codes, int8_t* V_codes,
+                           float* K_scales, float* V_scales, const int32_t* tables, const int32_t* start, const int32_t* n,
+                           int32_t* dev_status, void* stream);
+
+/*
+ * Verification attention over paged caches; what bass_verify_attention computes, with O [B, kmax, Hq, D] in bf16, as the output
+ * projection takes it.  The step's own K/V rows have been appended (bass_paged_append).
+ *
+ * bass_paged_attention_plan: the division of a step's work over the GPU, one small launch for all layers.
+ *   ctx_len, draft_len [B]    as in bass_verify_attention; ctx_len + draft_len <= max_pages * page_tokens (else clamped, BASS_STATUS_LEN_CLAMPED)
+ *   prefix_of [B] or NULL     number of the prefix a sequence begins with, negative: none
+ *   prefix_len [n_prefixes]   tokens of each prefix; n_prefixes <= 4096, 0 if prefix_of is NULL
+ * The tables of sequences with the same prefix must name the same pages for its tokens, as bass_page_tables makes them.  What is
+ * common to all of a prefix's sequences in this step (at most the shortest one's ctx_len, whole blocks of 32 tokens) is computed for all of
+ * them together where that is quicker; the result is that of separate sequences up to rounding.  Numbers outside [0, n_prefixes) count as none (from
+ * n_prefixes on with BASS_STATUS_LEN_CLAMPED).
+ * bass_paged_verify_attention: one layer.  tables [B, max_pages].  Page numbers outside the pool: page 0 is read in their place
+ * (BASS_STATUS_PAGE_CLAMPED).  A plan of another descriptor computes nothing (BASS_STATUS_PLAN_MISMATCH).  lse may be NULL.  kmax * (Hq / Hkv) <= 64.
+ * plan and workspace: device, 16-byte aligned, of at least the bytes the queries say; contents irrelevant on entry; calls that overlap must not share
+ * a workspace, and may share a plan.  Two launches.
+ */
+size_t bass_paged_attention_plan_bytes(const bass_paged_desc* desc);
+size_t bass_paged_attention_workspace_bytes(const bass_paged_desc* desc);
+int bass_paged_attention_plan(const bass_paged_desc* desc, const int32_t* ctx_len, const int32_t* draft_len, const int32_t* prefix_of,
+                              const int32_t* prefix_len, int32_t n_prefixes, void* plan, size_t plan_bytes, int32_t* dev_status,
+                              void* stream);
+int bass_paged_verify_attention(const bass_paged_desc* desc, const void* Q, const void* Kpool, const void* Vpool, const int32_t* tables,
+                                const void* plan, void* O, float* lse, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                                void* stream);
 
 /*
  * Draft-length heuristic (Algorithm 1 of the paper; HOST code, HOST pointers): picks the

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libbass.so")
 OK = 0
 ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE_TOO_SMALL, ERR_HIP = -1, -2, -3, -4
 STATUS_LEN_CLAMPED, STATUS_TOKEN_CLAMPED, STATUS_ZERO_MASS, STATUS_PLAN_MISMATCH = 1, 2, 4, 8
+STATUS_PAGE_CLAMPED, STATUS_NO_PAGES = 16, 32
 PLAN_APPEND = 1
 DTYPE_BF16, DTYPE_FP32, DTYPE_INT8KV = 0, 1, 2
 
@@ -29,6 +30,9 @@ EXPORTS = (
     "bass_set_attention_waves", "bass_draft_len_init", "bass_next_draft_len",
     "bass_attention_plan_bytes", "bass_attention_plan", "bass_attention_plan_host", "bass_verify_attention_planned",
     "bass_bench_stream_read", "bass_verify_attention_noalloc",
+    "bass_page_pool_bytes", "bass_page_tables_workspace_bytes", "bass_page_tables", "bass_paged_append", "bass_paged_gather",
+    "bass_paged_gather_int8", "bass_paged_attention_plan_bytes", "bass_paged_attention_workspace_bytes", "bass_paged_attention_plan",
+    "bass_paged_verify_attention",
 )
 
 
@@ -41,6 +45,18 @@ class AttnDesc(ctypes.Structure):
         vals = {f: getattr(self, f) for f, _ in self._fields_}
         vals.update(kw)
         return AttnDesc(**vals)
+
+
+class PagedDesc(ctypes.Structure):
+    """Mirror of `bass_paged_desc`."""
+    _fields_ = [("B", ctypes.c_int32), ("kmax", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+    def replace(self, **kw):
+        vals = {f: getattr(self, f) for f, _ in self._fields_}
+        vals.update(kw)
+        return PagedDesc(**vals)
 
 
 class DraftLenState(ctypes.Structure):
@@ -119,6 +135,23 @@ def lib():
         L.bass_bench_stream_read.argtypes = [vp, vp, sz, i32, vp, vp]
         L.bass_verify_attention_planned.restype = ctypes.c_int
         L.bass_verify_attention_planned.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+        pp = ctypes.POINTER(PagedDesc)
+        for name in ("bass_page_pool_bytes", "bass_paged_attention_plan_bytes", "bass_paged_attention_workspace_bytes"):
+            getattr(L, name).restype, getattr(L, name).argtypes = sz, [pp]
+        L.bass_page_tables_workspace_bytes.restype = sz
+        L.bass_page_tables_workspace_bytes.argtypes = [i32, i32]
+        L.bass_page_tables.restype = ctypes.c_int
+        L.bass_page_tables.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp, vp]
+        L.bass_paged_append.restype = ctypes.c_int
+        L.bass_paged_append.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp]
+        L.bass_paged_gather.restype = ctypes.c_int
+        L.bass_paged_gather.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.bass_paged_gather_int8.restype = ctypes.c_int
+        L.bass_paged_gather_int8.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.bass_paged_attention_plan.restype = ctypes.c_int
+        L.bass_paged_attention_plan.argtypes = [pp, vp, vp, vp, vp, i32, vp, sz, vp, vp]
+        L.bass_paged_verify_attention.restype = ctypes.c_int
+        L.bass_paged_verify_attention.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
         _lib = L
     return _lib
 
@@ -465,7 +498,160 @@ def bass_warp_accept(logits_main, logits_draft, temperature, top_p, draft_tok, n
         "bass_warp_accept")
 
 
+# ---- paged caches ------------------------------------------------------------------------------
+
+def make_paged_desc(B, kmax, Hq, Hkv, D, page_tokens, n_pages, max_pages, dtype, scale) -> PagedDesc:
+    code = {"bf16": DTYPE_BF16, "fp32": DTYPE_FP32, "int8kv": DTYPE_INT8KV}.get(dtype, dtype)
+    return PagedDesc(int(B), int(kmax), int(Hq), int(Hkv), int(D), int(page_tokens), int(n_pages), int(max_pages), int(code), float(scale))
+
+
+def bass_page_pool_bytes(desc: PagedDesc) -> int:
+    return int(lib().bass_page_pool_bytes(ctypes.byref(desc)))
+
+
+def bass_page_tables_workspace_bytes(rows, n_pages) -> int:
+    return int(lib().bass_page_tables_workspace_bytes(int(rows), int(n_pages)))
+
+
+def bass_paged_attention_plan_bytes(desc: PagedDesc) -> int:
+    return int(lib().bass_paged_attention_plan_bytes(ctypes.byref(desc)))
+
+
+def bass_paged_attention_workspace_bytes(desc: PagedDesc) -> int:
+    return int(lib().bass_paged_attention_workspace_bytes(ctypes.byref(desc)))
+
+
+def _bytes_of(t, need, name):
+    """Device pointer of a contiguous GPU tensor of any type that holds at least `need` bytes."""
+    if _nbytes(t, name) < need:
+        raise ValueError(f"{name} holds {_nbytes(t, name)} bytes, {need} are needed")
+    return t.data_ptr()
+
+
+def _pool_ptrs(Kpool, Vpool, desc):
+    need = lib().bass_page_pool_bytes(ctypes.byref(desc))
+    return _bytes_of(Kpool, need, "Kpool"), _bytes_of(Vpool, need, "Vpool")
+
+
+def _launch_on(stream, anchor, *others):
+    """The stream of a call on `anchor`'s device.  All tensors have to be there, and it has to be the current device, whose stream a
+    launch goes to."""
+    index = anchor.get_device()
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise ValueError("all tensors of a call must live on the same GPU")
+    if index != _torch()._C._cuda_getDevice():
+        raise ValueError("the tensors must live on the current GPU (torch.cuda.device)")
+    return _stream(stream)
+
+
+def bass_page_tables(length, held, tables, refs, page_tokens, workspace, share_from=None, share_len=None, ctx_len=None, n_new=None, slots=None,
+                     dev_status=None, stream=None):
+    """Pages taken, shared and given back for the rows' lengths (held [rows], tables [rows, max_pages], refs [n_pages] in place); slots [rows, kmax]
+    of the tokens ctx_len + i, i < n_new, where asked for."""
+    i32 = _torch().int32
+    if tables is None or tables.dim() != 2 or refs is None or refs.dim() != 1:
+        raise ValueError("tables must be [rows, max_pages] and refs [n_pages]")
+    if slots is not None and (slots.dim() != 2 or ctx_len is None or n_new is None):
+        raise ValueError("slots must be [rows, kmax] and needs ctx_len and n_new")
+    rows, max_pages = tables.shape
+    n_pages, kmax = refs.shape[0], 0 if slots is None else slots.shape[1]
+    one = (rows,)
+    args = (_dev(length, "length", i32, one), _dev(share_from, "share_from", i32, one, optional=True),
+            _dev(share_len, "share_len", i32, one, optional=True), _dev(held, "held", i32, one), _dev(tables, "tables", i32),
+            _dev(refs, "refs", i32), kmax, _dev(ctx_len, "ctx_len", i32, one, optional=True), _dev(n_new, "n_new", i32, one, optional=True),
+            _dev(slots, "slots", i32, (rows, kmax), optional=True))
+    ws = _bytes_of(workspace, 0, "workspace")
+    _check(lib().bass_page_tables(
+        rows, max_pages, int(page_tokens), n_pages, *args, ws, _nbytes(workspace, "workspace"),
+        _dev(dev_status, "dev_status", i32, optional=True),
+        _launch_on(stream, tables, length, share_from, share_len, held, refs, ctx_len, n_new, slots, workspace, dev_status)), "bass_page_tables")
+
+
+def bass_paged_append(desc, Kpool, Vpool, K_new, V_new, slots, dev_status=None, stream=None):
+    torch = _torch()
+    rows = (desc.B, desc.kmax, desc.Hkv, desc.D)
+    _check(lib().bass_paged_append(
+        ctypes.byref(desc), *_pool_ptrs(Kpool, Vpool, desc), _dev(K_new, "K_new", torch.bfloat16, rows), _dev(V_new, "V_new", torch.bfloat16, rows),
+        _dev(slots, "slots", torch.int32, rows[:2]), _dev(dev_status, "dev_status", torch.int32, optional=True),
+        _launch_on(stream, Kpool, Vpool, K_new, V_new, slots, dev_status)), "bass_paged_append")
+
+
+def _gather_args(desc, tables, start, n):
+    i32 = _torch().int32
+    return (_dev(tables, "tables", i32, (desc.B, desc.max_pages)), _dev(start, "start", i32, (desc.B,)), _dev(n, "n", i32, (desc.B,)))
+
+
+def bass_paged_gather(desc, Kpool, Vpool, K_out, V_out, tables, start, n, dev_status=None, stream=None):
+    torch = _torch()
+    rows = (desc.B, desc.kmax, desc.Hkv, desc.D)
+    _check(lib().bass_paged_gather(
+        ctypes.byref(desc), *_pool_ptrs(Kpool, Vpool, desc), _dev(K_out, "K_out", torch.bfloat16, rows), _dev(V_out, "V_out", torch.bfloat16, rows),
+        *_gather_args(desc, tables, start, n), _dev(dev_status, "dev_status", torch.int32, optional=True),
+        _launch_on(stream, Kpool, Vpool, K_out, V_out, tables, start, n, dev_status)), "bass_paged_gather")
+
+
+def bass_paged_gather_int8(desc, Kpool, Vpool, K_codes, V_codes, K_scales, V_scales, tables, start, n, dev_status=None, stream=None):
+    torch = _torch()
+    rows = (desc.B, desc.kmax, desc.Hkv, desc.D)
+    _check(lib().bass_paged_gather_int8(
+        ctypes.byref(desc), *_pool_ptrs(Kpool, Vpool, desc), _dev(K_codes, "K_codes", torch.int8, rows), _dev(V_codes, "V_codes", torch.int8, rows),
+        _dev(K_scales, "K_scales", torch.float32, rows[:3]), _dev(V_scales, "V_scales", torch.float32, rows[:3]),
+        *_gather_args(desc, tables, start, n), _dev(dev_status, "dev_status", torch.int32, optional=True),
+        _launch_on(stream, Kpool, Vpool, K_codes, V_codes, K_scales, V_scales, tables, start, n, dev_status)), "bass_paged_gather_int8")
+
+
+def bass_paged_attention_plan(desc, ctx_len, draft_len, prefix_of, prefix_len, plan, dev_status=None, stream=None):
+    """prefix_of [B] (negative: none) and prefix_len [n_prefixes], or None for both: nothing is shared."""
+    i32 = _torch().int32
+    if (prefix_of is None) != (prefix_len is None):
+        raise ValueError("prefix_of and prefix_len go together")
+    if prefix_len is not None and (prefix_len.dim() != 1 or prefix_len.shape[0] == 0):
+        raise ValueError("prefix_len must be [n_prefixes]")
+    one, need = (desc.B,), bass_paged_attention_plan_bytes(desc)
+    _check(lib().bass_paged_attention_plan(
+        ctypes.byref(desc), _dev(ctx_len, "ctx_len", i32, one), _dev(draft_len, "draft_len", i32, one),
+        _dev(prefix_of, "prefix_of", i32, one, optional=True), _dev(prefix_len, "prefix_len", i32, optional=True),
+        0 if prefix_len is None else prefix_len.shape[0], _bytes_of(plan, need, "plan"), _nbytes(plan, "plan"),
+        _dev(dev_status, "dev_status", i32, optional=True),
+        _launch_on(stream, plan, ctx_len, draft_len, prefix_of, prefix_len, dev_status)), "bass_paged_attention_plan")
+
+
+def bass_paged_verify_attention(desc, Q, Kpool, Vpool, tables, plan, O, lse, workspace, dev_status=None, stream=None):
+    torch = _torch()
+    q = (desc.B, desc.kmax, desc.Hq, desc.D)
+    _check(lib().bass_paged_verify_attention(
+        ctypes.byref(desc), _dev(Q, "Q", torch.bfloat16, q), *_pool_ptrs(Kpool, Vpool, desc),
+        _dev(tables, "tables", torch.int32, (desc.B, desc.max_pages)), _bytes_of(plan, bass_paged_attention_plan_bytes(desc), "plan"),
+        _dev(O, "O", torch.bfloat16, q), _dev(lse, "lse", torch.float32, q[:3], optional=True),
+        _bytes_of(workspace, 0, "workspace"), _nbytes(workspace, "workspace"), _dev(dev_status, "dev_status", torch.int32, optional=True),
+        _launch_on(stream, Q, Kpool, Vpool, tables, plan, O, lse, workspace, dev_status)), "bass_paged_verify_attention")
+
+
 # ---- allocation helpers (plumbing; no arithmetic) ----------------------------------------------
+
+def alloc_page_pool(desc, device="cuda", fill_byte=None):
+    """One pool (K or V) as a byte tensor; optionally filled with a byte pattern."""
+    t = _torch().empty(bass_page_pool_bytes(desc), dtype=_torch().uint8, device=device)
+    if fill_byte is not None:
+        t.fill_(fill_byte)
+    return t
+
+
+def alloc_paged_plan(desc, device="cuda"):
+    """A plan buffer of the attention over paged caches (bass_paged_attention_plan fills it)."""
+    return _torch().empty(bass_paged_attention_plan_bytes(desc), dtype=_torch().uint8, device=device)
+
+
+def alloc_paged_workspace(desc, device="cuda"):
+    """Workspace of the attention over paged caches (it needs no clearing)."""
+    return _torch().empty(bass_paged_attention_workspace_bytes(desc), dtype=_torch().uint8, device=device)
+
+
+def alloc_page_tables_workspace(rows, n_pages, device="cuda"):
+    """Workspace of bass_page_tables (it needs no clearing)."""
+    return _torch().empty(bass_page_tables_workspace_bytes(rows, n_pages), dtype=_torch().uint8, device=device)
+
 
 def alloc_kv_cache(desc, device="cuda", fill_byte=None):
     """One cache (K or V) as an opaque byte tensor; optionally filled with a byte pattern."""

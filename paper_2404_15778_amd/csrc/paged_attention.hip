@@ -1,0 +1,409 @@
+// Attention over paged caches with shared prefixes: bass_paged_verify_attention.
+//
+// A run's query tokens (paged_plan.h) see its blocks through one table.  Over a run of P, for a query row q:
+//   m = max_j s_j,  l = sum_j 2^(s_j - m),  a = sum_j 2^(s_j - m) v_j,   s_j = q k_j * scale * log2(e)   (one pass, 32 bits)
+// and a row's result over the runs and workgroups that have a part of its tokens: M = max m, O = sum 2^(m - M) a / sum 2^(m - M) l.
+// A prefix's blocks are so read once for the query rows of all sequences that begin with it.
+//
+// paged_attn: a workgroup of four wavefronts per share of the list.  The wavefronts take a unit's blocks in turn, each with the state of all of the
+// unit's query rows, NT tiles of 32 (wide_tiles.h), and merge their states through LDS at the end of the unit.
+// paged_merge: joins the partial results and writes O, lse and the zeros of unused rows.
+#include "paged_plan.h"
+#include "wide_tiles.h"
+
+namespace bass {
+
+constexpr int kPagedWaves = 4;
+
+struct PagedParams {
+  int B, kmax, Hq, Hkv, g, blocks_per_page, n_pages, max_pages;
+  unsigned g_magic;  // ceil(2^20 / g): r / g == (r * g_magic) >> 20 for r < 2048, g <= 64
+  float scale_log2;
+  int32_t signature;
+  const uint16_t* Q;
+  const uint4 *Kp, *Vp;
+  const int32_t* tables;
+  const PagedHeader* header;
+  const PagedShare* shares;
+  const PagedRun* runs;
+  const PagedSeq* seqs;
+  const int32_t* tokens;
+  uint16_t* O;
+  float* lse;
+  float* part_acc;  // [partial row][D]
+  float* part_ml;   // [partial row][2]: running maximum (log2 units), sum
+  int32_t* status;
+};
+
+// What a workgroup has of one unit.
+struct PagedSegment {
+  PagedRun run;
+  int kvh, tile;
+  int first, n;        // blocks
+  int tok, n_tok;      // query tokens: entries of the token list or, in a run of one sequence, tokens
+  bool solo;           // its result is the final one
+};
+
+__device__ inline PagedRun uniform_run(const PagedRun* at) {
+  PagedRun r = *at;
+  int* w = (int*)&r;
+#pragma unroll
+  for (size_t i = 0; i < sizeof(PagedRun) / 4; ++i) w[i] = uniform(w[i]);
+  return r;
+}
+
+__device__ inline PagedSegment paged_segment(const PagedRun& r, int unit, int off, int entries) {
+  PagedSegment s;
+  s.run = r;
+  s.kvh = unit / r.n_tiles;
+  s.tile = unit - s.kvh * r.n_tiles;
+  const int n = min(r.n_blk - off, entries);
+  s.first = r.first + off;
+  s.n = max(n, 0);
+  s.tok = r.tok + s.tile * r.tile_tok;
+  s.n_tok = min(r.tile_tok, r.n_tok - s.tile * r.tile_tok);
+  s.solo = r.whole && s.n == r.n_blk;
+  return s;
+}
+
+__device__ inline int row_of(const PagedParams& p, int r) { return (int)(((unsigned)r * p.g_magic) >> 20); }  // query token of a tile's row
+
+// Query token of a tile's row (any for a row that does not exist), as a row of [B * kmax].
+__device__ inline int token_of(const PagedParams& p, const PagedSegment& s, int row) {
+  const int t = row_of(p, row), at = s.tok + (t < s.n_tok ? t : 0);
+  return s.run.L < 0 ? p.tokens[at] : at;
+}
+
+// Operand B of the score tiles.  A lane's row is c of each tile, and its two lanes (h) have the row's 16-byte chunks in turn.  A negative softmax
+// scale is moved into the queries (exact), and so is a zero; the factor that is left is positive.  INT8: quantized like cached rows.
+template <int D, bool kI8, int NT>
+__device__ inline void load_paged_queries(const PagedParams& p, const PagedSegment& s, int c, int h, WideQueries<D, kI8, NT>& q) {
+  using G = Wide<D, kI8, NT>;
+  const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = 32 * nt + c, t = row_of(p, row);
+    const bool live = t < s.n_tok && p.scale_log2 != 0.f;
+    const int hg = row - t * p.g;
+    const u32x4* src = (const u32x4*)(p.Q + ((size_t)token_of(p, s, row) * p.Hq + s.kvh * p.g + hg) * D);
+    q.lim[nt] = s.run.L < 0 ? 0x7fffffff : s.run.L + (t < s.n_tok ? t : 0);
+    const uint32_t keep = live ? 0xFFFFFFFFu : 0u;
+    if constexpr (kI8) {
+      u32x4 raw[2 * G::kQuerySteps];
+      float amax = 0.f;
+#pragma unroll
+      for (int x = 0; x < 2 * G::kQuerySteps; ++x) {
+        raw[x] = (src[2 * (2 * (x >> 1) + h) + (x & 1)] ^ flip) & keep;
+        amax = fmaxf(amax, amax8(__builtin_bit_cast(uint4, raw[x])));
+      }
+      amax = G::row_max(amax);
+      const float scale = amax / 127.0f * fabsf(p.scale_log2);
+      const float inv = amax > 0.f && scale != 0.f ? 127.0f / amax : 0.f;
+      q.row_scale[nt] = scale != 0.f ? scale : 1.f;
+#pragma unroll
+      for (int x = 0; x < G::kQuerySteps; ++x) {
+        const uint2 lo = quantize8(__builtin_bit_cast(uint4, raw[2 * x]), inv), hi = quantize8(__builtin_bit_cast(uint4, raw[2 * x + 1]), inv);
+        q.q[nt][x] = u32x4{lo.x, lo.y, hi.x, hi.y};
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < G::kQuerySteps; ++x) q.q[nt][x] = (src[2 * x + h] ^ flip) & keep;
+    }
+  }
+}
+
+__device__ inline uint2 to_bf16(f32x4 v) {  // round to nearest even
+  typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+  return __builtin_bit_cast(uint2, __builtin_convertvector(v, bf16x4));
+}
+
+// Page numbers of the blocks that a wavefront takes, 64 at a time: lane l holds the block (counted over the pool's pages) of turn base + l.
+struct PageWindow {
+  int base;
+  int now, next;
+};
+
+template <int D, bool kI8, int NT>
+struct PagedExchange {
+  using G = Wide<D, kI8, NT>;
+  f32x4 acc[NT * G::kAcc][kPagedWaves - 1][4][64];
+  float m[kPagedWaves][NT][32], l[kPagedWaves][NT][32];
+  __align__(16) float scales[kPagedWaves][kI8 ? 64 : 4];
+};
+
+template <int D, bool kI8, int NT>
+__device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, int wg, PagedExchange<D, kI8, NT>& lds) {
+  using G = Wide<D, kI8, NT>;
+  using Block = WideBlock<D, kI8>;
+  constexpr int W = kPagedWaves, kAccs = NT * G::kAcc, kBlkVec = G::kBlkVec;
+  constexpr int R = 2;  // blocks a wavefront has in its registers or on the way there
+  const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
+  const int n_mine = (s.n - wv + W - 1) / W;  // turns of this wavefront: block s.first + wv + W t
+  const int32_t* table = p.tables + (size_t)s.run.row * p.max_pages;
+  int bad = 0;
+  auto pool_blocks = [&](int t0) {  // of turns t0 + lane
+    const int t = min(t0 + lane, max(n_mine - 1, 0)), blk = s.first + min(wv + W * t, s.n - 1);
+    const int at = blk / p.blocks_per_page;
+    int page = table[at];
+    if (page < 0 || page >= p.n_pages) {
+      page = 0;
+      bad = 1;
+    }
+    return page * p.blocks_per_page + (blk - at * p.blocks_per_page);
+  };
+  PageWindow win{0, pool_blocks(0), 0};
+  const int k_lane = 16 * G::k_lane(lane), v_lane = 16 * G::v_lane(lane);
+  // One past the end goes through a buffer descriptor of size zero and touches nothing: all fetches are unconditional (exact wait counts).
+  auto block_at = [&](int t) {
+    const int blk = t - win.base < 64 ? __builtin_amdgcn_readlane(win.now, (t - win.base) & 63) : __builtin_amdgcn_readlane(win.next, (t - win.base) & 63);
+    return pool_block(blk, p.blocks_per_page, p.Hkv, s.kvh) * kBlkVec;
+  };
+  auto fetch_k = [&](Block& r, int t) {
+    const size_t off = block_at(t);
+    const __amdgpu_buffer_rsrc_t at = dev_buffer((const float*)(p.Kp + off), t < n_mine ? 16u * kBlkVec : 0u);
+#pragma unroll
+    for (int x = 0; x < Block::kChunks; ++x) r.k[x] = __builtin_amdgcn_raw_buffer_load_b128(at, k_lane, 16 * G::k_step(x), kAuxNonTemporal);
+    if constexpr (kI8) r.scale = ((const float*)((lane < 32 ? p.Kp : p.Vp) + off + 2 * D))[lane % 32];
+  };
+  auto fetch_v = [&](Block& r, int t) {
+    const __amdgpu_buffer_rsrc_t at = dev_buffer((const float*)(p.Vp + block_at(t)), t < n_mine ? 16u * kBlkVec : 0u);
+#pragma unroll
+    for (int x = 0; x < Block::kChunks; ++x) r.v[x] = __builtin_amdgcn_raw_buffer_load_b128(at, v_lane, 16 * G::v_step(x), kAuxNonTemporal);
+  };
+  Block ring[R];
+#pragma unroll
+  for (int x = 0; x < R; ++x) {
+    fetch_k(ring[x], x);
+    fetch_v(ring[x], x);
+  }
+  WideQueries<D, kI8, NT> q;
+  load_paged_queries<D, kI8, NT>(p, s, c, h, q);
+  WideState<D, kI8, NT> st;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    st.m[nt] = -INFINITY;
+    st.l[nt] = 0.f;
+#pragma unroll
+    for (int a = 0; a < G::kAcc; ++a)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st.acc[nt][a][i] = 0.f;
+  }
+  const float abs_scale = p.scale_log2 == 0.f ? 1.f : fabsf(p.scale_log2);
+  const int n_valid = s.run.L < 0 ? 0x7fffffff : s.run.L + s.run.n_tok;  // tokens of the sequence
+  const int n_plain = s.run.L < 0 ? 0x7fffffff : s.run.L + 1;            // tokens that every row sees
+  auto step = [&](Block& r, int t) {
+    const int tok0 = (s.first + wv + W * t) * kBlockTokens;
+    float* sc = lds.scales[wv];
+    if constexpr (kI8) {
+      sc[lane] = (lane >= 32 && tok0 + lane - 32 >= n_valid) ? 0.f : r.scale;  // stale tokens may carry any V scale
+      __builtin_amdgcn_wave_barrier();  // a wavefront's LDS accesses stay in order
+    }
+    float z[NT][G::kScores];
+    wide_scores<D, kI8, NT>(r, q, abs_scale, h, sc, z);
+    fetch_k(r, t + R);
+    if (tok0 + kBlockTokens > n_plain) mask_wide<D, kI8, NT>(r, z, q, tok0, n_valid, h);
+    bf16x8 pf[NT][G::kProbs], pr[2][NT][G::kProbs];
+    wide_softmax<D, kI8, NT>(z, st, h, sc, pf, pr);
+    if constexpr (kI8) __builtin_amdgcn_wave_barrier();
+    wide_values<D, kI8, NT>(r, pf, pr, st);
+    fetch_v(r, t + R);
+  };
+  for (int t = 0; t < n_mine; t += R) {
+    if (t - win.base == 64) {  // on to the next window
+      win.base = t;
+      win.now = win.next;
+    }
+    if (t - win.base == 32 && t + 32 < n_mine) win.next = pool_blocks(t + 32);
+#pragma unroll
+    for (int x = 0; x < R; ++x) {
+      if (x > 0 && t + x >= n_mine) break;
+      step(ring[x], t + x);
+    }
+  }
+  if (bad && p.status) atomicOr(p.status, BASS_STATUS_PAGE_CLAMPED);
+
+  // The four states: M = max m_w, weights 2^(m_w - M) (a wavefront that saw no visible token has m = -inf and weight 0).
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const float l = G::row_sum(st.l[nt]);
+    if (h == 0) {
+      lds.m[wv][nt][c] = st.m[nt];
+      lds.l[wv][nt][c] = l;
+    }
+  }
+  __syncthreads();
+  float M[NT], sum[NT], mine[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    M[nt] = -INFINITY;
+    sum[nt] = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) M[nt] = fmaxf(M[nt], lds.m[w][nt][c]);
+    const float Mf = M[nt] == -INFINITY ? 0.f : M[nt];
+#pragma unroll
+    for (int w = 0; w < W; ++w) sum[nt] += lds.l[w][nt][c] * __builtin_amdgcn_exp2f(lds.m[w][nt][c] - Mf);
+    mine[nt] = __builtin_amdgcn_exp2f(st.m[nt] - Mf);
+  }
+  auto quad = [&](int x, int y) {
+    const typename G::Acc& a = st.acc[x / G::kAcc][x % G::kAcc];
+    return f32x4{a[4 * y], a[4 * y + 1], a[4 * y + 2], a[4 * y + 3]};
+  };
+#pragma unroll
+  for (int x = 0; x < kAccs; ++x) {
+    const int owner = x % W;
+    st.acc[x / G::kAcc][x % G::kAcc] *= mine[x / G::kAcc];
+    if (wv != owner) {
+#pragma unroll
+      for (int y = 0; y < 4; ++y) lds.acc[x][wv < owner ? wv : wv - 1][y][lane] = quad(x, y);
+    }
+  }
+  __syncthreads();
+  const size_t base = partial_row(s.run, p.g, s.kvh, s.tile, wg);
+#pragma unroll
+  for (int x = 0; x < kAccs; ++x) {
+    const int nt = x / G::kAcc, a = x % G::kAcc;
+    if (wv != x % W) continue;
+    const int row = 32 * nt + c, t = row_of(p, row);
+    f32x4 v[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      v[y] = quad(x, y);
+#pragma unroll
+      for (int w = 0; w < W - 1; ++w) v[y] += lds.acc[x][w][y][lane];
+    }
+    if (t < s.n_tok) {
+      if (s.solo) {
+        const size_t orow = (size_t)(s.tok + t) * p.Hq + s.kvh * p.g + (row - t * p.g);
+        const float inv = __builtin_amdgcn_rcpf(sum[nt]);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) *(uint2*)(p.O + orow * D + G::elem(a, y, h)) = to_bf16(v[y] * inv);
+        if (a == 0 && h == 0 && p.lse) p.lse[orow] = (M[nt] + __builtin_amdgcn_logf(sum[nt])) * 0.6931471805599453f;
+      } else {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) *(f32x4*)(p.part_acc + (base + row) * D + G::elem(a, y, h)) = v[y];
+        if (a == 0 && h == 0) *(float2*)(p.part_ml + (base + row) * 2) = make_float2(M[nt], sum[nt]);
+      }
+    }
+  }
+}
+
+template <int D, bool kI8>
+__global__ __launch_bounds__(64 * kPagedWaves, 1) void paged_attn(PagedParams p) {
+  __shared__ union {
+    PagedExchange<D, kI8, 1> one;
+    PagedExchange<D, kI8, 2> two;
+  } lds;
+  const PagedShare* rec = p.shares + blockIdx.x;
+  if (uniform(rec->signature) != p.signature) {
+    if (blockIdx.x == 0 && threadIdx.x == 0 && p.status) atomicOr(p.status, BASS_STATUS_PLAN_MISMATCH);
+    return;
+  }
+  int entries = uniform(rec->entries), run_no = uniform(rec->run), unit = uniform(rec->unit), off = uniform(rec->off);
+  if (entries <= 0) return;
+  PagedRun run = uniform_run(&rec->first);
+  for (;;) {
+    const PagedSegment s = paged_segment(run, unit, off, entries);
+    if (s.n > 0) {
+      if (s.n_tok * p.g <= 32) paged_unit<D, kI8, 1>(p, s, blockIdx.x, lds.one);
+      else paged_unit<D, kI8, 2>(p, s, blockIdx.x, lds.two);
+    }
+    entries -= run.n_blk + kPagedPad - off;
+    if (entries <= 0) break;
+    off = 0;
+    if (++unit == p.Hkv * run.n_tiles) {
+      unit = 0;
+      run = uniform_run(p.runs + ++run_no);
+    }
+    __syncthreads();  // the exchange is free again, whichever of its two forms is next
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Merge.  D / 4 threads per output row, four head elements each; a row's partial results are few (a unit's blocks are cut where
+// workgroups end, and there is at most one shared run).
+// ---------------------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256) void paged_merge(PagedParams p) {
+  constexpr int kLanes = D / 4;
+  if (uniform(p.header->signature) != p.signature) return;
+  const size_t orow = (size_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;  // over [B][kmax][Hq]
+  const int q4 = threadIdx.x % kLanes;
+  if (orow >= (size_t)p.B * p.kmax * p.Hq) return;
+  const int hq = (int)(orow % p.Hq), tok = (int)(orow / p.Hq), b = tok / p.kmax, i = tok - b * p.kmax;
+  const int kvh = hq / p.g, hg = hq - kvh * p.g;
+  const PagedSeq seq = p.seqs[b];
+  uint16_t* out = p.O + orow * D + 4 * q4;
+  if (i >= seq.nq) {
+    *(uint2*)out = make_uint2(0u, 0u);
+    if (p.lse && q4 == 0) p.lse[orow] = 0.f;
+    return;
+  }
+  const PagedSplit split{p.header->per, p.header->rem, p.header->total};
+  float M = -INFINITY, L = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  auto fold = [&](const PagedRun& r, int tile, int row) {
+    const int start = r.start + (kvh * r.n_tiles + tile) * (r.n_blk + kPagedPad);
+    const int w0 = split.owner(start), w1 = split.owner(start + r.n_blk - 1);
+    if (r.whole && w0 == w1) return false;  // written by the workgroup that has it all
+    for (int w = w0; w <= w1; ++w) {
+      const size_t at = partial_row(r, p.g, kvh, tile, w) + row;
+      const float2 ml = *(const float2*)(p.part_ml + at * 2);
+      const f32x4 a = *(const f32x4*)(p.part_acc + at * D + 4 * q4);
+      const float Mn = fmaxf(M, ml.x), Mf = Mn == -INFINITY ? 0.f : Mn;
+      const float wa = __builtin_amdgcn_exp2f(M - Mf), wb = __builtin_amdgcn_exp2f(ml.x - Mf);
+      L = L * wa + ml.y * wb;
+      acc = acc * wa + a * wb;
+      M = Mn;
+    }
+    return true;
+  };
+  if (seq.shared >= 0) {
+    const PagedRun& r = p.runs[seq.shared];
+    const int at = seq.pos + i, tile = at / r.tile_tok;
+    fold(r, tile, (at - tile * r.tile_tok) * p.g + hg);
+  }
+  if (!fold(p.runs[seq.own], 0, i * p.g + hg)) return;
+  const float inv = __builtin_amdgcn_rcpf(L);
+  *(uint2*)out = to_bf16(acc * inv);
+  if (p.lse && q4 == 0) p.lse[orow] = (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
+}
+
+}  // namespace bass
+
+extern "C" size_t bass_paged_attention_workspace_bytes(const bass_paged_desc* d) {
+  if (bass::check_paged_attention(d) != BASS_OK) return 0;
+  return bass::partial_rows(d) * (d->D + 2) * sizeof(float);
+}
+
+extern "C" int bass_paged_verify_attention(const bass_paged_desc* d, const void* Q, const void* Kpool, const void* Vpool, const int32_t* tables,
+                                           const void* plan, void* O, float* lse, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                                           void* stream) {
+  using namespace bass;
+  const int rc = check_paged_attention(d);
+  if (rc != BASS_OK) return rc;
+  if (!Q || !Kpool || !Vpool || !tables || !plan || !O || !workspace) return BASS_ERR_INVALID_ARG;
+  if (!aligned16(Q) || !aligned16(Kpool) || !aligned16(Vpool) || !aligned16(plan) || !aligned16(O) || !aligned16(workspace)) return BASS_ERR_INVALID_ARG;
+  if (workspace_bytes < bass_paged_attention_workspace_bytes(d)) return BASS_ERR_WORKSPACE_TOO_SMALL;
+  const PagedLayout l = paged_layout(d);
+  const char* at = (const char*)plan;
+  const int g = d->Hq / d->Hkv;
+  PagedParams p{d->B, d->kmax, d->Hq, d->Hkv, g, d->page_tokens / kBlockTokens, d->n_pages, d->max_pages, ((1u << 20) + g - 1) / g,
+                d->scale * 1.4426950408889634f, paged_signature(d), (const uint16_t*)Q, (const uint4*)Kpool, (const uint4*)Vpool, tables,
+                (const PagedHeader*)at, (const PagedShare*)(at + l.shares), (const PagedRun*)(at + l.runs), (const PagedSeq*)(at + l.seqs),
+                (const int32_t*)(at + l.tokens), (uint16_t*)O, lse, (float*)workspace, (float*)workspace + partial_rows(d) * d->D, dev_status};
+  hipStream_t s = (hipStream_t)stream;
+  const bool int8 = d->dtype == BASS_DTYPE_INT8KV;
+  const dim3 grid(kPagedShares), block(64 * kPagedWaves);
+  const int64_t rows = (int64_t)d->B * d->kmax * d->Hq;
+  const dim3 merge_grid((unsigned)((rows + 1024 / d->D - 1) / (1024 / d->D)));
+  if (d->D == 128) {
+    if (int8) hipLaunchKernelGGL((paged_attn<128, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((paged_attn<128, false>), grid, block, 0, s, p);
+    hipLaunchKernelGGL(paged_merge<128>, merge_grid, dim3(256), 0, s, p);
+  } else {
+    if (int8) hipLaunchKernelGGL((paged_attn<64, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((paged_attn<64, false>), grid, block, 0, s, p);
+    hipLaunchKernelGGL(paged_merge<64>, merge_grid, dim3(256), 0, s, p);
+  }
+  return launch_status();
+}

@@ -1,0 +1,100 @@
+// Work plan of the attention over paged caches: which blocks every workgroup takes, for which query rows.
+//
+// A run is a stretch of blocks that some query tokens see together: the common prefix of several sequences, with the query tokens of
+// all of them, or the rest of one sequence, with its own.  A run's query tokens are cut into tiles, and every (kv head, tile) of a run is a
+// unit of the run's n_blk blocks.  All units are laid end to end, each with kPagedPad virtual blocks behind it (the cost of its end: states
+// merged, a partial result stored), and the list is divided evenly over the workgroups.  Units of a shared run are in the order of the kv heads:
+// the tiles of a kv head read the same blocks, on the same XCD at about the same time.
+#pragma once
+#include "paged.h"
+
+namespace bass {
+
+constexpr int kPagedShares = 256;   // workgroups of the attention launch: one per compute unit
+constexpr int kPagedPad = 6;
+constexpr int kLeastEntries = 8;    // of a workgroup, as long as there are fewer workgroups than kPagedShares
+constexpr int kTileRows = 64;       // most query rows of a tile
+constexpr int kSlotRows = kTileRows;  // rows between the partial results of two workgroups (see partial_row)
+constexpr int kLeastShared = 4;     // a common prefix of fewer blocks is left to the sequences themselves
+
+struct PagedRun {
+  int32_t row;       // whose table is read
+  int32_t tok;       // shared: first entry of the token list; else: first query token b * kmax
+  int32_t n_tok;     // query tokens
+  int32_t tile_tok;  // query tokens of a tile
+  int32_t n_tiles;
+  int32_t first;     // first block
+  int32_t n_blk;     // blocks
+  int32_t L;         // tokens cached before the step; -1: shared (all of it is visible to all rows)
+  int32_t start;     // entries of the list before this run
+  int32_t row_base;  // partial rows before this run
+  int32_t whole;     // 1: the sequence has no shared part, so a unit that is not cut is the final result
+  int32_t reserved;
+};
+
+struct PagedHeader {
+  int32_t signature, n_runs, total, per, rem, used;
+  int32_t reserved[10];
+};
+
+// What a workgroup starts with; it goes on through the units (and runs) that follow until its entries are used up.
+struct PagedShare {
+  int32_t signature, run, unit, off, entries;  // first run, unit of the run, entry of the unit
+  int32_t reserved[3];
+  PagedRun first;  // the run itself: one trip to memory less
+};
+
+// A sequence, for the merge of its rows.
+struct PagedSeq {
+  int32_t nq, own, shared, pos;  // query tokens; its run; the shared run or -1; its first token's place in that run
+};
+
+struct PagedLayout {
+  size_t shares, runs, seqs, tokens, bytes;
+};
+inline PagedLayout paged_layout(const bass_paged_desc* d) {
+  PagedLayout l;
+  l.shares = sizeof(PagedHeader);
+  l.runs = l.shares + sizeof(PagedShare) * kPagedShares;
+  l.seqs = l.runs + sizeof(PagedRun) * 2 * (size_t)d->B;  // a shared run has two sequences at least
+  l.tokens = l.seqs + sizeof(PagedSeq) * (size_t)d->B;
+  l.bytes = (l.tokens + 4 * (size_t)d->B * d->kmax + 15) / 16 * 16;
+  return l;
+}
+
+// Even division of `total` entries over `used` shares.
+struct PagedSplit {
+  int per, rem, total;
+  BASS_HD int first(int w) const { return imin(w * per + imin(w, rem), total); }
+  BASS_HD int owner(int x) const {
+    const int big = rem * (per + 1);
+    return x < big ? x / (per + 1) : rem + (x - big) / imax(per, 1);
+  }
+};
+
+// Place of a unit's first row among the partial results of workgroup w.  Workgroups and units both come in the order of the list: with
+// the next pair of them at least a unit's rows, or kSlotRows, are added, so that no two pairs overlap.
+BASS_HD inline size_t partial_row(const PagedRun& r, int g, int kvh, int tile, int w) {
+  return (size_t)r.row_base + (size_t)kvh * r.n_tok * g + (size_t)tile * r.tile_tok * g + (size_t)w * kSlotRows;
+}
+inline size_t partial_rows(const bass_paged_desc* d) { return 2 * (size_t)d->B * d->kmax * d->Hq + (size_t)kPagedShares * kSlotRows; }
+
+inline int32_t paged_signature(const bass_paged_desc* d) {
+  uint32_t h = 2166136261u;
+  const int32_t v[] = {d->B, d->kmax, d->Hq, d->Hkv, d->D, d->page_tokens, d->max_pages, d->dtype, kPagedShares, kTileRows};
+  for (int32_t x : v)
+    for (int i = 0; i < 4; ++i) h = (h ^ ((uint32_t)x >> (8 * i) & 0xFFu)) * 16777619u;
+  return (int32_t)(h | 1u);  // never the zero of an empty buffer
+}
+
+inline int check_paged_attention(const bass_paged_desc* d) {
+  const int rc = check_paged(d);
+  if (rc != BASS_OK) return rc;
+  if (d->B > kMaxPagedBatch || (int64_t)d->kmax * (d->Hq / d->Hkv) > 64) return BASS_ERR_UNSUPPORTED;
+  // the list counts in 32 bits: every sequence's blocks, and at most as many again of shared runs
+  const int64_t blocks = (int64_t)d->max_pages * (d->page_tokens / kBlockTokens) + kPagedPad;
+  if (2 * blocks * d->B * d->Hkv >= (1ll << 31) || 2 * (int64_t)d->B * d->kmax * d->Hq >= (1ll << 31)) return BASS_ERR_UNSUPPORTED;
+  return BASS_OK;
+}
+
+}  // namespace bass

@@ -1,0 +1,202 @@
+// Planning of a step's attention over paged caches: bass_paged_attention_plan.
+//
+// One workgroup, everything but the results in LDS.  Phases: lengths; the prefixes' sequences, query tokens and common blocks; prefix sums over
+// the runs (shared ones first); the shared runs' token lists, in the order of the sequences; one record per workgroup of the attention launch.
+#include "paged_plan.h"
+
+namespace bass {
+
+constexpr int kPlanThreads2 = 1024;
+
+struct PagedPlanParams {
+  int B, kmax, g, Hkv, most_tokens, n_prefixes;
+  int32_t signature;
+  const int32_t *ctx_len, *draft_len, *prefix_of, *prefix_len;
+  PagedHeader* header;
+  PagedShare* shares;
+  PagedRun* runs;
+  PagedSeq* seqs;
+  int32_t* tokens;
+  int32_t* status;
+};
+
+// Exclusive prefix sum over the workgroup and its total; all threads call.
+__device__ inline int scan1024(int v, int* lds, int& total) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int t = __shfl_up(x, o);
+    if (lane >= o) x += t;
+  }
+  __syncthreads();
+  if (lane == 63) lds[wv] = x;
+  __syncthreads();
+  total = 0;
+  for (int i = 0; i < kPlanThreads2 / 64; ++i) {
+    if (i < wv) x += lds[i];
+    total += lds[i];
+  }
+  return x - v;
+}
+
+__global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanParams p) {
+  __shared__ int sums[kPlanThreads2 / 64];
+  __shared__ int seq_L[kMaxPagedBatch], seq_n[kMaxPagedBatch], seq_g[kMaxPagedBatch];
+  // of each prefix: least ctx_len, then common blocks; query tokens, then their first place in the list; sequences, then its run; first sequence
+  __shared__ int pre_L[kMaxPagedBatch], pre_tok[kMaxPagedBatch], pre_row[kMaxPagedBatch], pre_n[kMaxPagedBatch];
+  __shared__ int starts[2 * kMaxPagedBatch];
+  const int tid = threadIdx.x;
+  for (int x = tid; x < p.n_prefixes; x += kPlanThreads2) {
+    pre_L[x] = p.prefix_len[x];
+    pre_tok[x] = pre_n[x] = 0;
+    pre_row[x] = 1 << 30;
+  }
+  __syncthreads();
+  int bad = 0;
+  for (int b = tid; b < p.B; b += kPlanThreads2) {
+    int L = p.ctx_len[b], n = p.draft_len[b];
+    if (clamp_lengths(L, n, p.kmax, p.most_tokens)) bad = BASS_STATUS_LEN_CLAMPED;
+    int x = p.prefix_of ? p.prefix_of[b] : -1;
+    if (x >= p.n_prefixes) bad = BASS_STATUS_LEN_CLAMPED;
+    if (x < 0 || x >= p.n_prefixes || n == 0) x = -1;
+    seq_L[b] = L;
+    seq_n[b] = n;
+    seq_g[b] = x;
+    if (x >= 0) {
+      atomicMin(&pre_L[x], L);
+      atomicAdd(&pre_tok[x], n);
+      atomicMin(&pre_row[x], b);
+      atomicAdd(&pre_n[x], 1);
+    }
+  }
+  if (bad && p.status) atomicOr(p.status, bad);
+  __syncthreads();
+  // common blocks of a prefix's sequences; 0: they go by themselves
+  for (int x = tid; x < p.n_prefixes; x += kPlanThreads2)
+    pre_L[x] = pre_n[x] >= 2 && pre_L[x] >= kLeastShared * kBlockTokens ? pre_L[x] / kBlockTokens : 0;
+  __syncthreads();
+
+  // Runs: item x < n_prefixes is a prefix, the others are the sequences.
+  int n_runs = 0, entries = 0, rows = 0, listed = 0;
+  const int items = p.n_prefixes + p.B;
+  for (int x0 = 0; x0 < items; x0 += kPlanThreads2) {
+    const int x = x0 + tid, b = x - p.n_prefixes;
+    PagedRun r{};
+    int units = 0, list = 0;
+    if (x < p.n_prefixes) {
+      r.n_blk = pre_L[x];
+      if (r.n_blk > 0) {
+        r.row = pre_row[x];
+        r.n_tok = list = pre_tok[x];
+        r.n_tiles = (r.n_tok * p.g + kTileRows - 1) / kTileRows;
+        r.tile_tok = min((r.n_tok + r.n_tiles - 1) / r.n_tiles, kTileRows / p.g);
+        r.n_tiles = (r.n_tok + r.tile_tok - 1) / r.tile_tok;
+        r.L = -1;
+        units = r.n_tiles * p.Hkv;
+      }
+    } else if (x < items && seq_n[b] > 0) {
+      r.row = b;
+      r.tok = b * p.kmax;
+      r.n_tok = r.tile_tok = seq_n[b];
+      r.n_tiles = 1;
+      r.L = seq_L[b];
+      const int shared = seq_g[b] >= 0 ? pre_L[seq_g[b]] : 0;
+      r.first = shared;
+      r.n_blk = num_blocks(seq_L[b] + seq_n[b]) - shared;
+      r.whole = shared == 0;
+      units = p.Hkv;
+    }
+    int total;
+    const int at = n_runs + scan1024(units > 0, sums, total);
+    n_runs += total;
+    r.start = entries + scan1024(units * (r.n_blk + kPagedPad), sums, total);
+    entries += total;
+    r.row_base = rows + scan1024(units > 0 ? r.n_tok * p.g * p.Hkv : 0, sums, total);
+    rows += total;
+    const int place = listed + scan1024(list, sums, total);
+    listed += total;
+    if (x < p.n_prefixes) {
+      r.tok = place;
+      pre_n[x] = units > 0 ? at : -1;
+      pre_tok[x] = place;
+    }
+    if (units > 0) {
+      p.runs[at] = r;
+      starts[at] = r.start;
+    }
+    if (x >= p.n_prefixes && x < items) p.seqs[b] = PagedSeq{seq_n[b], units > 0 ? at : -1, -1, 0};
+  }
+  __syncthreads();
+
+  // Token lists of the shared runs: a sequence's tokens stand behind those of the sequences before it.
+  for (int b = tid; b < p.B; b += kPlanThreads2) {
+    const int x = seq_g[b];
+    if (x < 0 || pre_n[x] < 0) continue;
+    int pos = 0;
+    for (int o = pre_row[x]; o < b; ++o)
+      if (seq_g[o] == x) pos += seq_n[o];
+    for (int i = 0; i < seq_n[b]; ++i) p.tokens[pre_tok[x] + pos + i] = b * p.kmax + i;
+    p.seqs[b].shared = pre_n[x];
+    p.seqs[b].pos = pos;
+  }
+
+  // Few entries go to fewer workgroups, so that each of a workgroup's four wavefronts has a block or two.
+  const int used = min(kPagedShares, max(1, entries / kLeastEntries));
+  const PagedSplit split{entries / used, entries % used, entries};
+  if (tid == 0) {
+    PagedHeader h{};
+    h.signature = p.signature;
+    h.n_runs = n_runs;
+    h.total = entries;
+    h.per = split.per;
+    h.rem = split.rem;
+    h.used = used;
+    *p.header = h;
+  }
+  for (int w = tid; w < kPagedShares; w += kPlanThreads2) {
+    PagedShare s{};
+    s.signature = p.signature;
+    const int x0 = w < used ? split.first(w) : entries, x1 = w < used ? split.first(w + 1) : entries;
+    s.entries = x1 - x0;
+    if (s.entries > 0) {
+      int lo = 0, hi = n_runs - 1;  // the last run that starts at x0 or before
+      while (lo < hi) {
+        const int m = (lo + hi + 1) >> 1;
+        if (starts[m] <= x0) lo = m;
+        else hi = m - 1;
+      }
+      s.run = lo;
+      s.first = p.runs[lo];
+      const int len = s.first.n_blk + kPagedPad;
+      s.unit = (x0 - s.first.start) / len;
+      s.off = (x0 - s.first.start) % len;
+    }
+    p.shares[w] = s;
+  }
+}
+
+}  // namespace bass
+
+extern "C" size_t bass_paged_attention_plan_bytes(const bass_paged_desc* d) {
+  return bass::check_paged_attention(d) == BASS_OK ? bass::paged_layout(d).bytes : 0;
+}
+
+extern "C" int bass_paged_attention_plan(const bass_paged_desc* d, const int32_t* ctx_len, const int32_t* draft_len, const int32_t* prefix_of,
+                                         const int32_t* prefix_len, int32_t n_prefixes, void* plan, size_t plan_bytes, int32_t* dev_status,
+                                         void* stream) {
+  using namespace bass;
+  const int rc = check_paged_attention(d);
+  if (rc != BASS_OK) return rc;
+  if (!ctx_len || !draft_len || !plan || !aligned16(plan) || n_prefixes < 0) return BASS_ERR_INVALID_ARG;
+  if ((prefix_of == nullptr) != (n_prefixes == 0) || (prefix_of == nullptr) != (prefix_len == nullptr)) return BASS_ERR_INVALID_ARG;
+  if (n_prefixes > kMaxPagedBatch) return BASS_ERR_UNSUPPORTED;
+  const PagedLayout l = paged_layout(d);
+  if (plan_bytes < l.bytes) return BASS_ERR_WORKSPACE_TOO_SMALL;
+  char* at = (char*)plan;
+  PagedPlanParams p{d->B, d->kmax, d->Hq / d->Hkv, d->Hkv, d->max_pages * d->page_tokens, n_prefixes, paged_signature(d),
+                    ctx_len, draft_len, prefix_of, prefix_len, (PagedHeader*)at, (PagedShare*)(at + l.shares), (PagedRun*)(at + l.runs),
+                    (PagedSeq*)(at + l.seqs), (int32_t*)(at + l.tokens), dev_status};
+  hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads2), 0, (hipStream_t)stream, p);
+  return launch_status();
+}

@@ -8,7 +8,9 @@ from __future__ import annotations
 import numpy as np
 import torch
 
-from . import (bass_kv_gather_int8, bass_warp_probs, bass_warp_accept, bass_warp_accept_workspace_bytes, AttnDesc, alloc_kv_cache, alloc_workspace, bass_append_verify_attention, bass_kv_append, bass_kv_gather,
+from . import (PagedDesc, alloc_page_pool, alloc_page_tables_workspace, alloc_paged_plan, alloc_paged_workspace, bass_page_tables,
+               bass_paged_append, bass_paged_attention_plan, bass_paged_gather, bass_paged_gather_int8, bass_paged_verify_attention, make_paged_desc,
+               bass_kv_gather_int8, bass_warp_probs, bass_warp_accept, bass_warp_accept_workspace_bytes, AttnDesc, alloc_kv_cache, alloc_workspace, bass_append_verify_attention, bass_kv_append, bass_kv_gather,
                bass_spec_accept, bass_verify_attention, bass_verify_attention_pad, bass_verify_attention_split, make_desc)
 
 
@@ -82,6 +84,67 @@ class DeviceAttention:
         bass_append_verify_attention(self.desc, Q, K_new, V_new, self.Kc, self.Vc, ctx_len, draft_len, self.O,
                                      self.lse if want_lse else None, self.ws, self.status)
         return self.O, self.lse
+
+
+class DevicePages:
+    """Pools, plan and workspace of one attention layer over paged caches."""
+
+    def __init__(self, B, kmax, Hq, Hkv, D, page_tokens, n_pages, max_pages, dtype, scale, device="cuda", poison=False):
+        self.desc: PagedDesc = make_paged_desc(B, kmax, Hq, Hkv, D, page_tokens, n_pages, max_pages, dtype, scale)
+        self.device = device
+        fill = 0xFF if poison else 0  # NaN in bf16 and in the scales of INT8 blocks
+        self.K = alloc_page_pool(self.desc, device, fill)
+        self.V = alloc_page_pool(self.desc, device, fill)
+        self.plan = alloc_paged_plan(self.desc, device)
+        self.ws = alloc_paged_workspace(self.desc, device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        if poison:
+            self.plan.fill_(0xA5)
+            self.ws.fill_(0xFF)
+        self.O = torch.full((B, kmax, Hq, D), float("nan"), dtype=torch.bfloat16, device=device)
+        self.lse = torch.full((B, kmax, Hq), float("nan"), dtype=torch.float32, device=device)
+
+    def append(self, K_rows, V_rows, slots):
+        """Rows [b, n, Hkv, D] to slots [b, n]."""
+        d = self.desc.replace(B=int(slots.shape[0]), kmax=int(slots.shape[1]))
+        bass_paged_append(d, self.K, self.V, K_rows, V_rows, slots, self.status)
+
+    def gather(self, tables, start, count, n):
+        d = self.desc.replace(B=int(tables.shape[0]), kmax=int(n))
+        rows = (d.B, d.kmax, d.Hkv, d.D)
+        if d.dtype == 2:
+            out = [torch.zeros(rows, dtype=torch.int8, device=self.device) for _ in range(2)]
+            out += [torch.zeros(rows[:3], dtype=torch.float32, device=self.device) for _ in range(2)]
+            bass_paged_gather_int8(d, self.K, self.V, *out, tables, start, count, self.status)
+        else:
+            out = [torch.zeros(rows, dtype=torch.bfloat16, device=self.device) for _ in range(2)]
+            bass_paged_gather(d, self.K, self.V, *out, tables, start, count, self.status)
+        return out
+
+    def verify(self, Q, tables, ctx_len, draft_len, prefix_of=None, prefix_len=None, want_lse=True):
+        bass_paged_attention_plan(self.desc, ctx_len, draft_len, prefix_of, prefix_len, self.plan, self.status)
+        bass_paged_verify_attention(self.desc, Q, self.K, self.V, tables, self.plan, self.O, self.lse if want_lse else None, self.ws, self.status)
+        return self.O, self.lse
+
+
+class DeviceTables:
+    """Page tables of `rows` rows over a pool of n_pages pages."""
+
+    def __init__(self, rows, max_pages, page_tokens, n_pages, device="cuda"):
+        self.page_tokens, self.device = page_tokens, device
+        self.held = torch.zeros(rows, dtype=torch.int32, device=device)
+        self.tables = torch.full((rows, max_pages), -1, dtype=torch.int32, device=device)
+        self.refs = torch.zeros(n_pages, dtype=torch.int32, device=device)
+        self.ws = alloc_page_tables_workspace(rows, n_pages, device).fill_(0xA5)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+
+    def update(self, length, share_from=None, share_len=None, ctx_len=None, n_new=None, kmax=0):
+        """Host lists in; returns the slots of the new tokens (on the device) where they are asked for."""
+        up = lambda x: None if x is None else i32(x, self.device)  # noqa: E731
+        slots = torch.full((len(length), kmax), -7, dtype=torch.int32, device=self.device) if ctx_len is not None else None
+        bass_page_tables(up(length), self.held, self.tables, self.refs, self.page_tokens, self.ws, up(share_from), up(share_len), up(ctx_len), up(n_new),
+                         slots, self.status)
+        return slots
 
 
 def i32(a, device="cuda"):
