@@ -45,11 +45,9 @@ struct PagedSegment {
 };
 
 __device__ inline PagedRun uniform_run(const PagedRun* at) {
-  PagedRun r = *at;
-  int* w = (int*)&r;
-#pragma unroll
-  for (size_t i = 0; i < sizeof(PagedRun) / 4; ++i) w[i] = uniform(w[i]);
-  return r;
+  const i32x4 a = ((const i32x4*)at)[0], b = ((const i32x4*)at)[1], c = ((const i32x4*)at)[2];
+  return PagedRun{uniform(a[0]), uniform(a[1]), uniform(a[2]), uniform(a[3]), uniform(b[0]), uniform(b[1]), uniform(b[2]), uniform(b[3]),
+                  uniform(c[0]), uniform(c[1]), uniform(c[2]), 0};
 }
 
 __device__ inline PagedSegment paged_segment(const PagedRun& r, int unit, int off, int entries) {
@@ -287,11 +285,207 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
   }
 }
 
+// ---------------------------------------------------------------------------------------
+// Many query rows (a shared prefix): a wavefront has 32 NT rows of its own, 128 NT in all, and all four go through the blocks together.  A block
+// is fetched once for the workgroup, into registers two blocks ahead, and from there into LDS one block ahead, in the operand order
+// that it has in the pool (INT8: V as bf16, so that the codes are widened once and not by every wavefront).  Every wavefront reads the whole block
+// from LDS, 16 KB for 32 NT matrix instructions; with NT = 2 that is half of what LDS can deliver in their time.
+// Every token of a shared run is visible to every row: there are no masks.
+// ---------------------------------------------------------------------------------------
+template <int D, bool kI8>
+struct TileBlock {
+  u32x4 k[kBlockTokens * D * (kI8 ? 1 : 2) / 16];
+  u32x4 v[kBlockTokens * D * 2 / 16];
+  __align__(16) float scales[kI8 ? 64 : 4];  // of K, then of V
+};
+
+template <int D, bool kI8, int NT>
+__device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, int wg, TileBlock<D, kI8> (&lds)[2]) {
+  using G = Wide<D, kI8, NT>;
+  using F = Wide<D, false, NT>;  // V in LDS is bf16
+  constexpr int kVec = kBlockTokens * D * (kI8 ? 1 : 2) / 16;  // uint4 of codes or elements per block and tensor
+  constexpr int kLoads = (kVec + 255) / 256;
+  static_assert(kVec == 128 || kVec == 256 || kVec == 512, "heads of 64 and 128");
+  constexpr int kPool = G::kBlkVec;
+  const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
+  const int32_t* table = p.tables + (size_t)s.run.row * p.max_pages;
+  int bad = 0;
+  auto pool_blocks = [&](int t0) {
+    const int blk = s.first + min(t0 + lane, s.n - 1), at = blk / p.blocks_per_page;
+    int page = table[at];
+    if (page < 0 || page >= p.n_pages) {
+      page = 0;
+      bad = 1;
+    }
+    return page * p.blocks_per_page + (blk - at * p.blocks_per_page);
+  };
+  PageWindow win{0, pool_blocks(0), 0};
+  // Whole rounds of 256 chunks (INT8 heads of 64: half of the threads have one).
+  constexpr bool kHalf = kVec < 256;
+  const int mine = kHalf ? tid & (kVec - 1) : tid;
+  struct Stage {
+    u32x4 k0, k1, v0, v1;
+    float scale;
+  } even, odd;
+  auto fetch = [&](Stage& r, int t) {  // past the end: the last block again
+    const int u = min(t, s.n - 1) - win.base;
+    const int blk = u < 64 ? __builtin_amdgcn_readlane(win.now, u & 63) : __builtin_amdgcn_readlane(win.next, u & 63);
+    const size_t off = pool_block(blk, p.blocks_per_page, p.Hkv, s.kvh) * kPool;
+    const u32x4 *kb = (const u32x4*)(p.Kp + off) + mine, *vb = (const u32x4*)(p.Vp + off) + mine;
+    r.k0 = kb[0];
+    if constexpr (kLoads == 2) r.k1 = kb[256];
+    r.v0 = vb[0];
+    if constexpr (kLoads == 2) r.v1 = vb[256];
+    if constexpr (kI8) r.scale = ((const float*)((lane < 32 ? p.Kp : p.Vp) + off + 2 * D))[lane % 32];
+  };
+  auto commit = [&](const Stage& r, TileBlock<D, kI8>& b) {
+    if constexpr (kI8) {  // chunk (d / 32, lane): head elements d % 32 and 16 + d % 32 of eight tokens
+      if (!kHalf || tid < kVec) {
+        b.k[mine] = r.k0;
+        b.v[128 * (mine / 64) + mine % 64] = __builtin_bit_cast(u32x4, codes_to_bf16(r.v0[0], r.v0[1]));
+        b.v[128 * (mine / 64) + 64 + mine % 64] = __builtin_bit_cast(u32x4, codes_to_bf16(r.v0[2], r.v0[3]));
+      }
+      if (tid < 64) b.scales[tid] = r.scale;
+    } else {
+      b.k[mine] = r.k0;
+      b.v[mine] = r.v0;
+      if constexpr (kLoads == 2) {
+        b.k[256 + mine] = r.k1;
+        b.v[256 + mine] = r.v1;
+      }
+    }
+  };
+  fetch(even, 0);
+  fetch(odd, 1);
+  // this wavefront's rows: tokens of the tile's list from row 32 NT wv on
+  const int row0 = 32 * NT * wv, rows = s.n_tok * p.g;
+  const bool active = row0 < rows;
+  WideQueries<D, kI8, NT> q;
+  load_paged_queries<D, kI8, NT>(p, s, row0 + c, h, q);
+  f32x16 acc[NT][F::kAcc];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    m[nt] = -INFINITY;
+    l[nt] = 0.f;
+#pragma unroll
+    for (int a = 0; a < F::kAcc; ++a)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[nt][a][i] = 0.f;
+  }
+  // Scores stay as the products give them; the factor to log2 units (positive: load_paged_queries) is applied to their difference from the
+  // row's reference maximum, which loses nothing however large they are.  INT8 scores have the factor in the rows' scales.
+  const float factor = kI8 ? 1.f : p.scale_log2 == 0.f ? 1.f : fabsf(p.scale_log2);
+  const int k_lane = G::k_lane(lane), v_lane = F::v_lane(lane);
+  auto step = [&](const TileBlock<D, kI8>& b) {
+    if (!active) return;
+    float z[NT][16];
+    if constexpr (kI8) {
+      i32x16 t[NT] = {};
+#pragma unroll
+      for (int x = 0; x < G::kQuerySteps; ++x) {
+        const i32x4 k = __builtin_bit_cast(i32x4, b.k[k_lane + G::k_step(x)]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) t[nt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(k, __builtin_bit_cast(i32x4, q.q[nt][x]), t[nt], 0, 0, 0);
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const f32x4 ks = *(const f32x4*)&b.scales[G::token(4 * y, h)];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[nt][4 * y + e] = (float)t[nt][4 * y + e] * (ks[e] * q.row_scale[nt]);
+      }
+    } else {
+      f32x16 t[NT] = {};
+#pragma unroll
+      for (int x = 0; x < G::kQuerySteps; ++x) {
+        const bf16x8 k = __builtin_bit_cast(bf16x8, b.k[k_lane + G::k_step(x)]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) t[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, q.q[nt][x]), t[nt], 0, 0, 0);
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[nt][i] = t[nt][i];
+    }
+    bf16x8 pf[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float mx = z[nt][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, z[nt][i]);
+      mx = F::row_max(mx);
+      const bool grow = (mx - m[nt]) * factor > kMaxSlack;  // from -inf: infinite
+      if (__any(grow)) {
+        const float m_new = grow ? mx : m[nt];
+        const float alpha = grow ? __builtin_amdgcn_exp2f((m[nt] - m_new) * factor) : 1.f;
+        l[nt] *= alpha;
+#pragma unroll
+        for (int a = 0; a < F::kAcc; ++a) acc[nt][a] *= alpha;
+        m[nt] = m_new;
+      }
+      const float m_use = m[nt] == -INFINITY ? 0.f : m[nt];  // no score above -inf yet
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = __builtin_amdgcn_exp2f((z[nt][i] - m_use) * factor);
+        sum += e;
+        if constexpr (kI8) pf[nt][i >> 3][i & 7] = (__bf16)(e * b.scales[32 + G::token(i, h)]);
+        else pf[nt][i >> 3][i & 7] = (__bf16)e;
+      }
+      l[nt] += sum;
+    }
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) {
+      const bf16x8 v = __builtin_bit_cast(bf16x8, b.v[v_lane + F::v_step(x)]);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) acc[nt][x >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[nt][x & 1], acc[nt][x >> 1], 0, 0, 0);
+    }
+  };
+  commit(even, lds[0]);
+  fetch(even, 2);
+  __syncthreads();
+  for (int t = 0; t < s.n; t += 2) {
+    if (t - win.base == 64) {
+      win.base = t;
+      win.now = win.next;
+    }
+    if (t - win.base == 32 && t + 32 < s.n) win.next = pool_blocks(t + 32);
+    commit(odd, lds[1]);  // block t + 1
+    fetch(odd, t + 3);
+    step(lds[0]);
+    __syncthreads();
+    if (t + 1 >= s.n) break;
+    commit(even, lds[0]);
+    fetch(even, t + 4);
+    step(lds[1]);
+    __syncthreads();
+  }
+  if (bad && p.status) atomicOr(p.status, BASS_STATUS_PAGE_CLAMPED);
+  if (!active) return;
+  const size_t base = partial_row(s.run, p.g, s.kvh, s.tile, wg);
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = row0 + 32 * nt + c;
+    const float sum = F::row_sum(l[nt]);
+    if (row < rows) {
+      if (h == 0) *(float2*)(p.part_ml + (base + row) * 2) = make_float2(m[nt] * factor, sum);
+#pragma unroll
+      for (int a = 0; a < F::kAcc; ++a)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          *(f32x4*)(p.part_acc + (base + row) * D + F::elem(a, y, h)) = f32x4{acc[nt][a][4 * y], acc[nt][a][4 * y + 1], acc[nt][a][4 * y + 2], acc[nt][a][4 * y + 3]};
+    }
+  }
+}
+
 template <int D, bool kI8>
 __global__ __launch_bounds__(64 * kPagedWaves, 1) void paged_attn(PagedParams p) {
   __shared__ union {
     PagedExchange<D, kI8, 1> one;
     PagedExchange<D, kI8, 2> two;
+    TileBlock<D, kI8> tile[2];
   } lds;
   const PagedShare* rec = p.shares + blockIdx.x;
   if (uniform(rec->signature) != p.signature) {
@@ -304,8 +498,11 @@ __global__ __launch_bounds__(64 * kPagedWaves, 1) void paged_attn(PagedParams p)
   for (;;) {
     const PagedSegment s = paged_segment(run, unit, off, entries);
     if (s.n > 0) {
-      if (s.n_tok * p.g <= 32) paged_unit<D, kI8, 1>(p, s, blockIdx.x, lds.one);
-      else paged_unit<D, kI8, 2>(p, s, blockIdx.x, lds.two);
+      const int rows = s.n_tok * p.g;
+      if (rows <= 32) paged_unit<D, kI8, 1>(p, s, blockIdx.x, lds.one);
+      else if (rows <= 64) paged_unit<D, kI8, 2>(p, s, blockIdx.x, lds.two);
+      else if (rows <= 128) paged_tile<D, kI8, 1>(p, s, blockIdx.x, lds.tile);
+      else paged_tile<D, kI8, 2>(p, s, blockIdx.x, lds.tile);
     }
     entries -= run.n_blk + kPagedPad - off;
     if (entries <= 0) break;

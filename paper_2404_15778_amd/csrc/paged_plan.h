@@ -13,7 +13,7 @@ namespace bass {
 constexpr int kPagedShares = 256;   // workgroups of the attention launch: one per compute unit
 constexpr int kPagedPad = 6;
 constexpr int kLeastEntries = 8;    // of a workgroup, as long as there are fewer workgroups than kPagedShares
-constexpr int kTileRows = 64;       // most query rows of a tile
+constexpr int kTileRows = 256;      // most query rows of a tile
 constexpr int kSlotRows = kTileRows;  // rows between the partial results of two workgroups (see partial_row)
 constexpr int kLeastShared = 4;     // a common prefix of fewer blocks is left to the sequences themselves
 
