@@ -323,7 +323,7 @@ typedef struct bass_paged_desc {
   int32_t kmax;        /* query-token slots per sequence                                                    */
   int32_t Hq, Hkv, D;  /* as in bass_attn_desc; D: 64 or 128                                                 */
   int32_t page_tokens; /* tokens of a page: a multiple of 32                                                 */
-  int32_t n_pages;     /* pages of a pool; n_pages * page_tokens < 2^31                                      */
+  int32_t n_pages;     /* pages of a pool; n_pages * page_tokens and n_pages * page_tokens / 32 * Hkv below 2^31 */
   int32_t max_pages;   /* entries of a sequence's table                                                      */
   int32_t dtype;       /* BASS_DTYPE_BF16 or BASS_DTYPE_INT8KV: the pools; Q, K_new, V_new and O are bf16     */
   float scale;

@@ -13,8 +13,9 @@ inline int check_paged(const bass_paged_desc* d) {
   if (d->Hq % d->Hkv != 0) return BASS_ERR_INVALID_ARG;
   if (d->dtype != BASS_DTYPE_BF16 && d->dtype != BASS_DTYPE_INT8KV) return BASS_ERR_UNSUPPORTED;
   if ((d->D != 64 && d->D != 128) || d->page_tokens % kBlockTokens != 0) return BASS_ERR_UNSUPPORTED;
-  // slots and tokens of a table are 32-bit numbers, and so are the blocks of a pool of one kv head
+  // slots, tokens of a table and blocks of a pool are 32-bit numbers
   if ((int64_t)d->n_pages * d->page_tokens >= (1ll << 31) || (int64_t)d->max_pages * d->page_tokens >= (1ll << 31)) return BASS_ERR_UNSUPPORTED;
+  if ((int64_t)d->n_pages * (d->page_tokens / kBlockTokens) * d->Hkv >= (1ll << 31)) return BASS_ERR_UNSUPPORTED;
   return BASS_OK;
 }
 

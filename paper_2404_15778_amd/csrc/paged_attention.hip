@@ -289,79 +289,100 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
 // Many query rows (a shared prefix): a wavefront has 32 NT rows of its own, 128 NT in all, and all four go through the blocks together.  A block
 // is fetched once for the workgroup, into registers two blocks ahead, and from there into LDS one block ahead, in the operand order
 // that it has in the pool (INT8: V as bf16, so that the codes are widened once and not by every wavefront).  Every wavefront reads the whole block
-// from LDS, 16 KB for 32 NT matrix instructions; with NT = 2 that is half of what LDS can deliver in their time.
+// from LDS, 16 KB for 16 NT matrix instructions; with NT = 2 that is half of what LDS can deliver in their time.
 // Every token of a shared run is visible to every row: there are no masks.
 // ---------------------------------------------------------------------------------------
 template <int D, bool kI8>
-struct TileBlock {
-  u32x4 k[kBlockTokens * D * (kI8 ? 1 : 2) / 16];
-  u32x4 v[kBlockTokens * D * 2 / 16];
-  __align__(16) float scales[kI8 ? 64 : 4];  // of K, then of V
+struct TileBlocks {
+  u32x4 k[2][kBlockTokens * D * (kI8 ? 1 : 2) / 16];
+  u32x4 v[2][kBlockTokens * D * 2 / 16];
+  __align__(16) float scales[kI8 ? 4 : 1][64];  // of K, then of V; four blocks
 };
 
+// The order in which a half turn's instructions are laid down: after each of its n matrix instructions the part of the softmax and of the LDS
+// reads that fits beside it.
+template <int n, bool kReads, bool kI8>
+__device__ inline void interleave() {
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);         // matrix
+    if (kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
+    __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);         // exponential
+    __builtin_amdgcn_sched_group_barrier(0x002, kI8 ? 8 : 5, 0);  // vector
+  }
+}
+
 template <int D, bool kI8, int NT>
-__device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, int wg, TileBlock<D, kI8> (&lds)[2]) {
+__device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, int wg, TileBlocks<D, kI8>& lds) {
   using G = Wide<D, kI8, NT>;
   using F = Wide<D, false, NT>;  // V in LDS is bf16
-  constexpr int kVec = kBlockTokens * D * (kI8 ? 1 : 2) / 16;  // uint4 of codes or elements per block and tensor
+  constexpr int kVec = kBlockTokens * D * (kI8 ? 1 : 2) / 16;  // chunks of codes or elements per block and tensor
   constexpr int kLoads = (kVec + 255) / 256;
   static_assert(kVec == 128 || kVec == 256 || kVec == 512, "heads of 64 and 128");
   constexpr int kPool = G::kBlkVec;
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
   const int32_t* table = p.tables + (size_t)s.run.row * p.max_pages;
   int bad = 0;
-  auto pool_blocks = [&](int t0) {
+  auto pool_blocks = [&](int t0) {  // blocks t0 + lane, as the pool counts them
     const int blk = s.first + min(t0 + lane, s.n - 1), at = blk / p.blocks_per_page;
     int page = table[at];
     if (page < 0 || page >= p.n_pages) {
       page = 0;
       bad = 1;
     }
-    return page * p.blocks_per_page + (blk - at * p.blocks_per_page);
+    return (page * p.Hkv + s.kvh) * p.blocks_per_page + (blk - at * p.blocks_per_page);
   };
-  PageWindow win{0, pool_blocks(0), 0};
+  int now = pool_blocks(0), next = 0, base_t = 0;  // lane l: block base_t + l, base_t + 64 + l
   // Whole rounds of 256 chunks (INT8 heads of 64: half of the threads have one).
   constexpr bool kHalf = kVec < 256;
   const int mine = kHalf ? tid & (kVec - 1) : tid;
   struct Stage {
-    u32x4 k0, k1, v0, v1;
+    u32x4 a, b;
     float scale;
-  } even, odd;
-  auto fetch = [&](Stage& r, int t) {  // past the end: the last block again
-    const int u = min(t, s.n - 1) - win.base;
-    const int blk = u < 64 ? __builtin_amdgcn_readlane(win.now, u & 63) : __builtin_amdgcn_readlane(win.next, u & 63);
-    const size_t off = pool_block(blk, p.blocks_per_page, p.Hkv, s.kvh) * kPool;
-    const u32x4 *kb = (const u32x4*)(p.Kp + off) + mine, *vb = (const u32x4*)(p.Vp + off) + mine;
-    r.k0 = kb[0];
-    if constexpr (kLoads == 2) r.k1 = kb[256];
-    r.v0 = vb[0];
-    if constexpr (kLoads == 2) r.v1 = vb[256];
-    if constexpr (kI8) r.scale = ((const float*)((lane < 32 ? p.Kp : p.Vp) + off + 2 * D))[lane % 32];
+  } k_even, k_odd, v_even, v_odd;
+  auto block_of = [&](int t) { return __builtin_amdgcn_readlane(now, t & 63); };
+  auto fetch = [&](Stage& r, const uint4* pool, int blk) {
+    const u32x4* at = (const u32x4*)(pool + (size_t)blk * kPool) + mine;
+    r.a = at[0];
+    if constexpr (kLoads == 2) r.b = at[256];
   };
-  auto commit = [&](const Stage& r, TileBlock<D, kI8>& b) {
-    if constexpr (kI8) {  // chunk (d / 32, lane): head elements d % 32 and 16 + d % 32 of eight tokens
-      if (!kHalf || tid < kVec) {
-        b.k[mine] = r.k0;
-        b.v[128 * (mine / 64) + mine % 64] = __builtin_bit_cast(u32x4, codes_to_bf16(r.v0[0], r.v0[1]));
-        b.v[128 * (mine / 64) + 64 + mine % 64] = __builtin_bit_cast(u32x4, codes_to_bf16(r.v0[2], r.v0[3]));
-      }
-      if (tid < 64) b.scales[tid] = r.scale;
-    } else {
-      b.k[mine] = r.k0;
-      b.v[mine] = r.v0;
-      if constexpr (kLoads == 2) {
-        b.k[256 + mine] = r.k1;
-        b.v[256 + mine] = r.v1;
-      }
+  auto fetch_k = [&](Stage& r, int blk) {
+    fetch(r, p.Kp, blk);
+    if constexpr (kI8) r.scale = ((const float*)((lane < 32 ? p.Kp : p.Vp) + (size_t)blk * kPool + 2 * D))[lane % 32];
+  };
+  auto commit_k = [&](const Stage& r, int t) {
+    u32x4* to = lds.k[t & 1];
+    if (!kHalf || tid < kVec) to[mine] = r.a;
+    if constexpr (kLoads == 2) to[256 + mine] = r.b;
+    if constexpr (kI8) {
+      if (tid < 64) lds.scales[t & 3][tid] = r.scale;
     }
   };
-  fetch(even, 0);
-  fetch(odd, 1);
-  // this wavefront's rows: tokens of the tile's list from row 32 NT wv on
+  auto commit_v = [&](const Stage& r, int t) {
+    u32x4* to = lds.v[t & 1];
+    if constexpr (kI8) {  // chunk (d / 32, lane): head elements d % 32 and 16 + d % 32 of eight tokens
+      if (!kHalf || tid < kVec) {
+        to[128 * (mine / 64) + mine % 64] = __builtin_bit_cast(u32x4, codes_to_bf16(r.a[0], r.a[1]));
+        to[128 * (mine / 64) + 64 + mine % 64] = __builtin_bit_cast(u32x4, codes_to_bf16(r.a[2], r.a[3]));
+      }
+    } else {
+      to[mine] = r.a;
+      if constexpr (kLoads == 2) to[256 + mine] = r.b;
+    }
+  };
+  fetch_k(k_even, block_of(0));
+  fetch_k(k_odd, block_of(1));
+  fetch(v_even, p.Vp, block_of(0));
+  // This wavefront's rows: from row 32 NT wv of the tile on.  Rows that do not exist have zero queries and are not stored.
   const int row0 = 32 * NT * wv, rows = s.n_tok * p.g;
-  const bool active = row0 < rows;
   WideQueries<D, kI8, NT> q;
   load_paged_queries<D, kI8, NT>(p, s, row0 + c, h, q);
+  // The queries stay in accumulation registers, where matrix instructions take an operand from as they are: the others' room is needed.
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int x = 0; x < G::kQuerySteps; ++x) asm volatile("" : "+a"(q.q[nt][x]));
+  typedef typename std::conditional<kI8, i32x16, f32x16>::type Scores;
   f32x16 acc[NT][F::kAcc];
   float m[NT], l[NT];
 #pragma unroll
@@ -373,97 +394,164 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[nt][a][i] = 0.f;
   }
-  // Scores stay as the products give them; the factor to log2 units (positive: load_paged_queries) is applied to their difference from the
-  // row's reference maximum, which loses nothing however large they are.  INT8 scores have the factor in the rows' scales.
+  // bf16 scores stay as the products give them; the factor to log2 units (positive: load_paged_queries) is applied to their difference from
+  // the row's reference maximum, which loses nothing however large they are.  INT8 scores get the scales of row and token, multiplied first.
   const float factor = kI8 ? 1.f : p.scale_log2 == 0.f ? 1.f : fabsf(p.scale_log2);
   const int k_lane = G::k_lane(lane), v_lane = F::v_lane(lane);
-  auto step = [&](const TileBlock<D, kI8>& b) {
-    if (!active) return;
-    float z[NT][16];
-    if constexpr (kI8) {
-      i32x16 t[NT] = {};
+  constexpr int kSteps = G::kQuerySteps, kFrags = D / 16;
+  u32x4 kf[kSteps], vf[kFrags];  // operands of the block at hand: K of block t + 1, V of block t
+  Scores z[NT];
+  float e[NT][16];
+  bf16x8 pf[NT][2];
+  auto read_k = [&](int x, int t) { kf[x] = lds.k[t & 1][k_lane + G::k_step(x)]; };
+  auto read_v = [&](int x, int t) { vf[x] = lds.v[t & 1][v_lane + F::v_step(x)]; };
+  auto score = [&](int nt, int x) {
+    if (x == 0) z[nt] = Scores{};
+    if constexpr (kI8) z[nt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, kf[x]), __builtin_bit_cast(i32x4, q.q[nt][x]), z[nt], 0, 0, 0);
+    else z[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x]), __builtin_bit_cast(bf16x8, q.q[nt][x]), z[nt], 0, 0, 0);
+  };
+  auto value = [&](int nt, int x) {
+    acc[nt][x >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[x]), pf[nt][x & 1], acc[nt][x >> 1], 0, 0, 0);
+  };
+  // Block t's scores as numbers, and the largest of each row.
+  float mx[NT];
+  auto peak = [&](int nt, int t) {
 #pragma unroll
-      for (int x = 0; x < G::kQuerySteps; ++x) {
-        const i32x4 k = __builtin_bit_cast(i32x4, b.k[k_lane + G::k_step(x)]);
+    for (int y = 0; y < 4; ++y) {
+      if constexpr (kI8) {
+        const f32x4 ks = *(const f32x4*)&lds.scales[t & 3][G::token(4 * y, h)] * q.row_scale[nt];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) t[nt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(k, __builtin_bit_cast(i32x4, q.q[nt][x]), t[nt], 0, 0, 0);
+        for (int i = 0; i < 4; ++i) e[nt][4 * y + i] = (float)z[nt][4 * y + i] * ks[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[nt][4 * y + i] = z[nt][4 * y + i];
       }
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        const f32x4 ks = *(const f32x4*)&b.scales[G::token(4 * y, h)];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) z[nt][4 * y + e] = (float)t[nt][4 * y + e] * (ks[e] * q.row_scale[nt]);
-      }
-    } else {
-      f32x16 t[NT] = {};
-#pragma unroll
-      for (int x = 0; x < G::kQuerySteps; ++x) {
-        const bf16x8 k = __builtin_bit_cast(bf16x8, b.k[k_lane + G::k_step(x)]);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) t[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, q.q[nt][x]), t[nt], 0, 0, 0);
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) z[nt][i] = t[nt][i];
     }
-    bf16x8 pf[NT][2];
+    float x = e[nt][0];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      float mx = z[nt][0];
+    for (int i = 1; i < 16; ++i) x = fmaxf(x, e[nt][i]);
+    mx[nt] = F::row_max(x);
+  };
+  // The row's reference maximum moves when a block exceeds it by more than kMaxSlack.
+  auto settle = [&](int nt) {
+    const bool grow = (mx[nt] - m[nt]) * factor > kMaxSlack;  // from -inf: infinite
+    if (__any(grow)) {
+      const float m_new = grow ? mx[nt] : m[nt];
+      const float alpha = grow ? __builtin_amdgcn_exp2f((m[nt] - m_new) * factor) : 1.f;
+      l[nt] *= alpha;
 #pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, z[nt][i]);
-      mx = F::row_max(mx);
-      const bool grow = (mx - m[nt]) * factor > kMaxSlack;  // from -inf: infinite
-      if (__any(grow)) {
-        const float m_new = grow ? mx : m[nt];
-        const float alpha = grow ? __builtin_amdgcn_exp2f((m[nt] - m_new) * factor) : 1.f;
-        l[nt] *= alpha;
-#pragma unroll
-        for (int a = 0; a < F::kAcc; ++a) acc[nt][a] *= alpha;
-        m[nt] = m_new;
-      }
-      const float m_use = m[nt] == -INFINITY ? 0.f : m[nt];  // no score above -inf yet
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = __builtin_amdgcn_exp2f((z[nt][i] - m_use) * factor);
-        sum += e;
-        if constexpr (kI8) pf[nt][i >> 3][i & 7] = (__bf16)(e * b.scales[32 + G::token(i, h)]);
-        else pf[nt][i >> 3][i & 7] = (__bf16)e;
-      }
-      l[nt] += sum;
-    }
-#pragma unroll
-    for (int x = 0; x < D / 16; ++x) {
-      const bf16x8 v = __builtin_bit_cast(bf16x8, b.v[v_lane + F::v_step(x)]);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) acc[nt][x >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[nt][x & 1], acc[nt][x >> 1], 0, 0, 0);
+      for (int a = 0; a < F::kAcc; ++a) acc[nt][a] *= alpha;
+      m[nt] = m_new;
     }
   };
-  commit(even, lds[0]);
-  fetch(even, 2);
-  __syncthreads();
-  for (int t = 0; t < s.n; t += 2) {
-    if (t - win.base == 64) {
-      win.base = t;
-      win.now = win.next;
+  auto probabilities = [&](int nt, int t, bool counts) {
+    const float m_use = m[nt] == -INFINITY ? 0.f : m[nt];  // no score above -inf yet
+    float sum = 0.f;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      f32x4 vs = {1.f, 1.f, 1.f, 1.f};
+      if constexpr (kI8) vs = *(const f32x4*)&lds.scales[t & 3][32 + G::token(4 * y, h)];
+#pragma unroll
+      for (int i = 4 * y; i < 4 * y + 4; ++i) {
+        const float x = __builtin_amdgcn_exp2f(kI8 ? e[nt][i] - m_use : (e[nt][i] - m_use) * factor);
+        sum += x;
+        pf[nt][i >> 3][i & 7] = (__bf16)(kI8 ? x * vs[i & 3] : x);
+      }
     }
-    if (t - win.base == 32 && t + 32 < s.n) win.next = pool_blocks(t + 32);
-    commit(odd, lds[1]);  // block t + 1
-    fetch(odd, t + 3);
-    step(lds[0]);
-    __syncthreads();
+    l[nt] += counts ? sum : 0.f;
+    // here, not where they are needed: in front of the branch of settle()
+    asm volatile("" : "+v"(pf[nt][0]), "+v"(pf[nt][1]), "+v"(l[nt]));
+  };
+  // Two tiles of rows go through the blocks half a block apart, so that the matrix instructions of one stand beside the softmax of the
+  // other: turn t is  [scores of A, block t + 1; values of A, block t | probabilities of B, block t], then
+  // [scores of B, block t + 1; values of B, block t | probabilities of A, block t + 1].  Operands are read from LDS in the second half, each as soon
+  // as its last use is past.  The last turn's scores are of the last block again, and their probabilities are not counted.
+  int v_blk = 0;  // block t + 3
+  auto turn = [&](int t, Stage& k_stage, Stage& v_stage) {
+    const bool more = t + 1 < s.n;
+    const int k_blk = block_of(t + 4);
+    commit_k(k_stage, t + 2);
+    commit_v(v_stage, t + 1);
+    fetch_k(k_stage, k_blk);
+    fetch(v_stage, p.Vp, v_blk);
+    v_blk = k_blk;
+    if constexpr (NT == 2) {
+#pragma unroll
+      for (int x = 0; x < kSteps; ++x) score(0, x);
+#pragma unroll
+      for (int x = 0; x < kFrags; ++x) value(0, x);
+      probabilities(1, t, true);
+      peak(0, t + 1);
+      interleave<kSteps + kFrags, false, kI8>();
+      settle(0);
+      __syncthreads();
+#pragma unroll
+      for (int x = 0; x < kSteps; ++x) {
+        score(1, x);
+        read_k(x, t + 2);
+      }
+#pragma unroll
+      for (int x = 0; x < kFrags; ++x) {
+        value(1, x);
+        read_v(x, t + 1);
+      }
+      probabilities(0, t + 1, more);
+      peak(1, t + 1);
+      interleave<kSteps + kFrags, true, kI8>();
+      settle(1);
+    } else {
+      __syncthreads();
+#pragma unroll
+      for (int x = 0; x < kSteps; ++x) {
+        score(0, x);
+        read_k(x, t + 2);
+      }
+#pragma unroll
+      for (int x = 0; x < kFrags; ++x) {
+        value(0, x);
+        read_v(x, t + 1);
+      }
+      peak(0, t + 1);
+      settle(0);
+      probabilities(0, t + 1, more);
+    }
+  };
+  commit_k(k_even, 0);
+  commit_k(k_odd, 1);
+  commit_v(v_even, 0);
+  fetch_k(k_even, block_of(2));
+  fetch_k(k_odd, block_of(3));
+  fetch(v_even, p.Vp, block_of(1));
+  fetch(v_odd, p.Vp, block_of(2));
+  v_blk = block_of(3);
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < kSteps; ++x) {
+    read_k(x, 0);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) score(nt, x);
+    read_k(x, 1);
+  }
+#pragma unroll
+  for (int x = 0; x < kFrags; ++x) read_v(x, 0);
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    peak(nt, 0);
+    settle(nt);
+  }
+  probabilities(0, 0, true);
+  __syncthreads();  // before the first turn writes over block 0
+  for (int t = 0; t < s.n; t += 2) {
+    if (t + 4 - base_t == 64) {
+      base_t += 64;
+      now = next;
+    }
+    if (t + 4 - base_t == 32) next = pool_blocks(base_t + 64);
+    turn(t, k_even, v_even);
     if (t + 1 >= s.n) break;
-    commit(even, lds[0]);
-    fetch(even, t + 4);
-    step(lds[1]);
-    __syncthreads();
+    turn(t + 1, k_odd, v_odd);
   }
   if (bad && p.status) atomicOr(p.status, BASS_STATUS_PAGE_CLAMPED);
-  if (!active) return;
   const size_t base = partial_row(s.run, p.g, s.kvh, s.tile, wg);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -485,7 +573,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, 1) void paged_attn(PagedParams p)
   __shared__ union {
     PagedExchange<D, kI8, 1> one;
     PagedExchange<D, kI8, 2> two;
-    TileBlock<D, kI8> tile[2];
+    TileBlocks<D, kI8> tile;
   } lds;
   const PagedShare* rec = p.shares + blockIdx.x;
   if (uniform(rec->signature) != p.signature) {
