@@ -350,7 +350,7 @@ size_t bass_page_pool_bytes(const bass_paged_desc* desc);
  * row itself shares nothing (BASS_STATUS_LEN_CLAMPED).  Entries that are no page are neither shared nor counted (BASS_STATUS_PAGE_CLAMPED).
  * The result does not depend on the order in which anything runs.  rows, max_pages, n_pages > 0, page_tokens a multiple of 32, rows * max_pages < 2^31,
  * n_pages * page_tokens < 2^31, 0 <= kmax <= 65535.  workspace: device, 16-byte aligned, at least bass_page_tables_workspace_bytes(rows, n_pages) bytes,
- * contents irrelevant on entry.  Three launches.
+ * contents irrelevant on entry.  One launch for few rows of a small pool, else three or four.
  */
 size_t bass_page_tables_workspace_bytes(int32_t rows, int32_t n_pages);
 int bass_page_tables(int32_t rows, int32_t max_pages, int32_t page_tokens, int32_t n_pages, const int32_t* length,

@@ -5,15 +5,14 @@
 // and a row's result over the runs and workgroups that have a part of its tokens: M = max m, O = sum 2^(m - M) a / sum 2^(m - M) l.
 // A prefix's blocks are so read once for the query rows of all sequences that begin with it.
 //
-// paged_attn: a workgroup of four wavefronts per share of the list.  The wavefronts take a unit's blocks in turn, each with the state of all of the
-// unit's query rows, NT tiles of 32 (wide_tiles.h), and merge their states through LDS at the end of the unit.
+// paged_attn: a workgroup of four wavefronts per share of the list.  Up to 64 query rows: the wavefronts take a unit's blocks in turn, each with the
+// state of all of the unit's rows, NT tiles of 32 (wide_tiles.h), and merge their states through LDS at the end of the unit; in short runs each has a kv
+// head of its own.  More rows: every wavefront has rows of its own, and they go through the blocks together.
 // paged_merge: joins the partial results and writes O, lse and the zeros of unused rows.
 #include "paged_plan.h"
 #include "wide_tiles.h"
 
 namespace bass {
-
-constexpr int kPagedWaves = 4;
 
 struct PagedParams {
   int B, kmax, Hq, Hkv, g, blocks_per_page, n_pages, max_pages;
@@ -38,7 +37,7 @@ struct PagedParams {
 // What a workgroup has of one unit.
 struct PagedSegment {
   PagedRun run;
-  int kvh, tile;
+  int kvh, tile;       // (first) kv head
   int first, n;        // blocks
   int tok, n_tok;      // query tokens: entries of the token list or, in a run of one sequence, tokens
   bool solo;           // its result is the final one
@@ -46,18 +45,21 @@ struct PagedSegment {
 
 __device__ inline PagedRun uniform_run(const PagedRun* at) {
   const i32x4 a = ((const i32x4*)at)[0], b = ((const i32x4*)at)[1], c = ((const i32x4*)at)[2];
+  const int heads = ((const int*)at)[12];
   return PagedRun{uniform(a[0]), uniform(a[1]), uniform(a[2]), uniform(a[3]), uniform(b[0]), uniform(b[1]), uniform(b[2]), uniform(b[3]),
-                  uniform(c[0]), uniform(c[1]), uniform(c[2]), 0};
+                  uniform(c[0]), uniform(c[1]), uniform(c[2]), uniform(c[3]),
+                  uniform(heads), {0, 0, 0}};
 }
 
 __device__ inline PagedSegment paged_segment(const PagedRun& r, int unit, int off, int entries) {
   PagedSegment s;
   s.run = r;
-  s.kvh = unit / r.n_tiles;
-  s.tile = unit - s.kvh * r.n_tiles;
-  const int n = min(r.n_blk - off, entries);
-  s.first = r.first + off;
-  s.n = max(n, 0);
+  const int at = unit / r.n_tiles;
+  s.kvh = at * r.heads;
+  s.tile = unit - at * r.n_tiles;
+  const int from = r.block_at(off);
+  s.first = r.first + from;
+  s.n = (entries < r.n_blk * r.cost - off ? r.block_at(off + entries) : r.n_blk) - from;
   s.tok = r.tok + s.tile * r.tile_tok;
   s.n_tok = min(r.tile_tok, r.n_tok - s.tile * r.tile_tok);
   s.solo = r.whole && s.n == r.n_blk;
@@ -75,7 +77,7 @@ __device__ inline int token_of(const PagedParams& p, const PagedSegment& s, int 
 // Operand B of the score tiles.  A lane's row is c of each tile, and its two lanes (h) have the row's 16-byte chunks in turn.  A negative softmax
 // scale is moved into the queries (exact), and so is a zero; the factor that is left is positive.  INT8: quantized like cached rows.
 template <int D, bool kI8, int NT>
-__device__ inline void load_paged_queries(const PagedParams& p, const PagedSegment& s, int c, int h, WideQueries<D, kI8, NT>& q) {
+__device__ inline void load_paged_queries(const PagedParams& p, const PagedSegment& s, int kvh, int c, int h, WideQueries<D, kI8, NT>& q) {
   using G = Wide<D, kI8, NT>;
   const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
 #pragma unroll
@@ -83,7 +85,7 @@ __device__ inline void load_paged_queries(const PagedParams& p, const PagedSegme
     const int row = 32 * nt + c, t = row_of(p, row);
     const bool live = t < s.n_tok && p.scale_log2 != 0.f;
     const int hg = row - t * p.g;
-    const u32x4* src = (const u32x4*)(p.Q + ((size_t)token_of(p, s, row) * p.Hq + s.kvh * p.g + hg) * D);
+    const u32x4* src = (const u32x4*)(p.Q + ((size_t)token_of(p, s, row) * p.Hq + kvh * p.g + hg) * D);
     q.lim[nt] = s.run.L < 0 ? 0x7fffffff : s.run.L + (t < s.n_tok ? t : 0);
     const uint32_t keep = live ? 0xFFFFFFFFu : 0u;
     if constexpr (kI8) {
@@ -129,18 +131,22 @@ struct PagedExchange {
   __align__(16) float scales[kPagedWaves][kI8 ? 64 : 4];
 };
 
-template <int D, bool kI8, int NT>
+// kHeads: a wavefront has a kv head of its own and all of the blocks (run.heads).
+template <int D, bool kI8, int NT, bool kHeads>
 __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, int wg, PagedExchange<D, kI8, NT>& lds) {
   using G = Wide<D, kI8, NT>;
   using Block = WideBlock<D, kI8>;
   constexpr int W = kPagedWaves, kAccs = NT * G::kAcc, kBlkVec = G::kBlkVec;
   constexpr int R = 2;  // blocks a wavefront has in its registers or on the way there
+  constexpr int kStride = kHeads ? 1 : W;
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
-  const int n_mine = (s.n - wv + W - 1) / W;  // turns of this wavefront: block s.first + wv + W t
+  const int kvh = s.kvh + (kHeads ? wv : 0), first_mine = kHeads ? 0 : wv;
+  if (kHeads && kvh >= p.Hkv) return;
+  const int n_mine = (s.n - first_mine + kStride - 1) / kStride;  // turns of this wavefront: block s.first + first_mine + kStride t
   const int32_t* table = p.tables + (size_t)s.run.row * p.max_pages;
   int bad = 0;
   auto pool_blocks = [&](int t0) {  // of turns t0 + lane
-    const int t = min(t0 + lane, max(n_mine - 1, 0)), blk = s.first + min(wv + W * t, s.n - 1);
+    const int t = min(t0 + lane, max(n_mine - 1, 0)), blk = s.first + min(first_mine + kStride * t, s.n - 1);
     const int at = blk / p.blocks_per_page;
     int page = table[at];
     if (page < 0 || page >= p.n_pages) {
@@ -154,7 +160,7 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
   // One past the end goes through a buffer descriptor of size zero and touches nothing: all fetches are unconditional (exact wait counts).
   auto block_at = [&](int t) {
     const int blk = t - win.base < 64 ? __builtin_amdgcn_readlane(win.now, (t - win.base) & 63) : __builtin_amdgcn_readlane(win.next, (t - win.base) & 63);
-    return pool_block(blk, p.blocks_per_page, p.Hkv, s.kvh) * kBlkVec;
+    return pool_block(blk, p.blocks_per_page, p.Hkv, kvh) * kBlkVec;
   };
   auto fetch_k = [&](Block& r, int t) {
     const size_t off = block_at(t);
@@ -175,7 +181,7 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
     fetch_v(ring[x], x);
   }
   WideQueries<D, kI8, NT> q;
-  load_paged_queries<D, kI8, NT>(p, s, c, h, q);
+  load_paged_queries<D, kI8, NT>(p, s, kvh, c, h, q);
   WideState<D, kI8, NT> st;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -190,7 +196,7 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
   const int n_valid = s.run.L < 0 ? 0x7fffffff : s.run.L + s.run.n_tok;  // tokens of the sequence
   const int n_plain = s.run.L < 0 ? 0x7fffffff : s.run.L + 1;            // tokens that every row sees
   auto step = [&](Block& r, int t) {
-    const int tok0 = (s.first + wv + W * t) * kBlockTokens;
+    const int tok0 = (s.first + first_mine + kStride * t) * kBlockTokens;
     float* sc = lds.scales[wv];
     if constexpr (kI8) {
       sc[lane] = (lane >= 32 && tok0 + lane - 32 >= n_valid) ? 0.f : r.scale;  // stale tokens may carry any V scale
@@ -220,6 +226,37 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
   }
   if (bad && p.status) atomicOr(p.status, BASS_STATUS_PAGE_CLAMPED);
 
+  const size_t base = partial_row(s.run, p.g, kvh, s.tile, wg);
+  // A quad of head elements of row `row` (valid), and with the first one the row's maximum and sum: the result, or a partial one.
+  auto deliver = [&](int row, int d, f32x4 v, bool first, float M, float sum, float inv) {
+    if (s.solo) {
+      const int t = row_of(p, row);
+      const size_t orow = (size_t)(s.tok + t) * p.Hq + kvh * p.g + (row - t * p.g);
+      *(uint2*)(p.O + orow * D + d) = to_bf16(v * inv);
+      if (first && p.lse) p.lse[orow] = (M + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+    } else {
+      *(f32x4*)(p.part_acc + (base + row) * D + d) = v;
+      if (first) *(float2*)(p.part_ml + (base + row) * 2) = make_float2(M, sum);
+    }
+  };
+  auto quad = [&](int x, int y) {
+    const typename G::Acc& a = st.acc[x / G::kAcc][x % G::kAcc];
+    return f32x4{a[4 * y], a[4 * y + 1], a[4 * y + 2], a[4 * y + 3]};
+  };
+  if constexpr (kHeads) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float sum = G::row_sum(st.l[nt]), inv = __builtin_amdgcn_rcpf(sum);
+      const int row = 32 * nt + c;
+      if (row < s.n_tok * p.g) {
+#pragma unroll
+        for (int a = 0; a < G::kAcc; ++a)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) deliver(row, G::elem(a, y, h), quad(nt * G::kAcc + a, y), a == 0 && y == 0 && h == 0, st.m[nt], sum, inv);
+      }
+    }
+    return;
+  }
   // The four states: M = max m_w, weights 2^(m_w - M) (a wavefront that saw no visible token has m = -inf and weight 0).
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -242,10 +279,6 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
     for (int w = 0; w < W; ++w) sum[nt] += lds.l[w][nt][c] * __builtin_amdgcn_exp2f(lds.m[w][nt][c] - Mf);
     mine[nt] = __builtin_amdgcn_exp2f(st.m[nt] - Mf);
   }
-  auto quad = [&](int x, int y) {
-    const typename G::Acc& a = st.acc[x / G::kAcc][x % G::kAcc];
-    return f32x4{a[4 * y], a[4 * y + 1], a[4 * y + 2], a[4 * y + 3]};
-  };
 #pragma unroll
   for (int x = 0; x < kAccs; ++x) {
     const int owner = x % W;
@@ -256,12 +289,12 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
     }
   }
   __syncthreads();
-  const size_t base = partial_row(s.run, p.g, s.kvh, s.tile, wg);
 #pragma unroll
   for (int x = 0; x < kAccs; ++x) {
     const int nt = x / G::kAcc, a = x % G::kAcc;
     if (wv != x % W) continue;
-    const int row = 32 * nt + c, t = row_of(p, row);
+    const int row = 32 * nt + c;
+    const float inv = __builtin_amdgcn_rcpf(sum[nt]);
     f32x4 v[4];
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
@@ -269,18 +302,9 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
 #pragma unroll
       for (int w = 0; w < W - 1; ++w) v[y] += lds.acc[x][w][y][lane];
     }
-    if (t < s.n_tok) {
-      if (s.solo) {
-        const size_t orow = (size_t)(s.tok + t) * p.Hq + s.kvh * p.g + (row - t * p.g);
-        const float inv = __builtin_amdgcn_rcpf(sum[nt]);
+    if (row < s.n_tok * p.g) {
 #pragma unroll
-        for (int y = 0; y < 4; ++y) *(uint2*)(p.O + orow * D + G::elem(a, y, h)) = to_bf16(v[y] * inv);
-        if (a == 0 && h == 0 && p.lse) p.lse[orow] = (M[nt] + __builtin_amdgcn_logf(sum[nt])) * 0.6931471805599453f;
-      } else {
-#pragma unroll
-        for (int y = 0; y < 4; ++y) *(f32x4*)(p.part_acc + (base + row) * D + G::elem(a, y, h)) = v[y];
-        if (a == 0 && h == 0) *(float2*)(p.part_ml + (base + row) * 2) = make_float2(M[nt], sum[nt]);
-      }
+      for (int y = 0; y < 4; ++y) deliver(row, G::elem(a, y, h), v[y], a == 0 && y == 0 && h == 0, M[nt], sum[nt], inv);
     }
   }
 }
@@ -376,7 +400,7 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   // This wavefront's rows: from row 32 NT wv of the tile on.  Rows that do not exist have zero queries and are not stored.
   const int row0 = 32 * NT * wv, rows = s.n_tok * p.g;
   WideQueries<D, kI8, NT> q;
-  load_paged_queries<D, kI8, NT>(p, s, row0 + c, h, q);
+  load_paged_queries<D, kI8, NT>(p, s, s.kvh, row0 + c, h, q);
   // The queries stay in accumulation registers, where matrix instructions take an operand from as they are: the others' room is needed.
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
@@ -587,15 +611,17 @@ __global__ __launch_bounds__(64 * kPagedWaves, 1) void paged_attn(PagedParams p)
     const PagedSegment s = paged_segment(run, unit, off, entries);
     if (s.n > 0) {
       const int rows = s.n_tok * p.g;
-      if (rows <= 32) paged_unit<D, kI8, 1>(p, s, blockIdx.x, lds.one);
-      else if (rows <= 64) paged_unit<D, kI8, 2>(p, s, blockIdx.x, lds.two);
-      else if (rows <= 128) paged_tile<D, kI8, 1>(p, s, blockIdx.x, lds.tile);
+      if (rows <= 32 && run.heads > 1) paged_unit<D, kI8, 1, true>(p, s, blockIdx.x, lds.one);
+      else if (rows <= 32) paged_unit<D, kI8, 1, false>(p, s, blockIdx.x, lds.one);
+      else if (rows <= kWaveRows && run.heads > 1) paged_unit<D, kI8, 2, true>(p, s, blockIdx.x, lds.two);
+      else if (rows <= kWaveRows) paged_unit<D, kI8, 2, false>(p, s, blockIdx.x, lds.two);
+      else if (rows <= kTileRows / 2) paged_tile<D, kI8, 1>(p, s, blockIdx.x, lds.tile);
       else paged_tile<D, kI8, 2>(p, s, blockIdx.x, lds.tile);
     }
-    entries -= run.n_blk + kPagedPad - off;
+    entries -= run.entries() - off;
     if (entries <= 0) break;
     off = 0;
-    if (++unit == p.Hkv * run.n_tiles) {
+    if (++unit == (p.Hkv + run.heads - 1) / run.heads * run.n_tiles) {
       unit = 0;
       run = uniform_run(p.runs + ++run_no);
     }
@@ -604,50 +630,73 @@ __global__ __launch_bounds__(64 * kPagedWaves, 1) void paged_attn(PagedParams p)
 }
 
 // ---------------------------------------------------------------------------------------
-// Merge.  D / 4 threads per output row, four head elements each; a row's partial results are few (a unit's blocks are cut where
-// workgroups end, and there is at most one shared run).
+// Merge.  A workgroup per query token and 1024 / D of its heads, D / 4 threads per output row, four head elements each.  A row's partial results lie
+// wherever a workgroup ended inside its unit, of the shared run and of its own; kMergeRound of them are on their way at a time, because each
+// round is a trip to memory.  Latency: header and sequence, then the partial results.
 // ---------------------------------------------------------------------------------------
+constexpr int kMergeRound = 8;
+
 template <int D>
-__global__ __launch_bounds__(256) void paged_merge(PagedParams p) {
-  constexpr int kLanes = D / 4;
-  if (uniform(p.header->signature) != p.signature) return;
-  const size_t orow = (size_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;  // over [B][kmax][Hq]
-  const int q4 = threadIdx.x % kLanes;
-  if (orow >= (size_t)p.B * p.kmax * p.Hq) return;
-  const int hq = (int)(orow % p.Hq), tok = (int)(orow / p.Hq), b = tok / p.kmax, i = tok - b * p.kmax;
-  const int kvh = hq / p.g, hg = hq - kvh * p.g;
-  const PagedSeq seq = p.seqs[b];
+__global__ __launch_bounds__(256) void paged_merge(PagedParams p, int head_groups) {
+  constexpr int kLanes = D / 4, kRows = 256 / kLanes;
+  const int tok = blockIdx.x / head_groups, b = tok / p.kmax, i = tok - b * p.kmax;
+  const int hq = (int)(blockIdx.x % head_groups) * kRows + threadIdx.x / kLanes, q4 = threadIdx.x % kLanes;
+  const PagedHeader* header = p.header;
+  const PagedSeq* seq = p.seqs + b;
+  const int signature = uniform(header->signature), nq = uniform(seq->nq), pos = uniform(seq->pos);
+  const PagedSplit split{uniform(header->per), uniform(header->rem), uniform(header->total)};
+  const PagedRun own = uniform_run(&seq->own), shared = uniform_run(&seq->shared);
+  if (signature != p.signature || hq >= p.Hq) return;
+  const size_t orow = (size_t)tok * p.Hq + hq;
   uint16_t* out = p.O + orow * D + 4 * q4;
-  if (i >= seq.nq) {
+  if (i >= nq) {
     *(uint2*)out = make_uint2(0u, 0u);
     if (p.lse && q4 == 0) p.lse[orow] = 0.f;
     return;
   }
-  const PagedSplit split{p.header->per, p.header->rem, p.header->total};
+  const int kvh = hq / p.g, hg = hq - kvh * p.g;
+  // Partial results of a run: n of them from workgroup w0 on, kSlotRows rows apart.
+  auto parts = [&](const PagedRun& r, int tile, int row, int& n) {
+    const int start = r.start + (kvh / r.heads * r.n_tiles + tile) * r.entries();
+    const int w0 = split.owner(start);
+    n = split.owner(start + (r.n_blk - 1) * r.cost) - w0 + 1;
+    return partial_row(r, p.g, kvh, tile, w0) + row;
+  };
+  int n_own, n_shared = 0;
+  const size_t at_own = parts(own, 0, i * p.g + hg, n_own);
+  if (own.whole && n_own == 1) return;  // written by the workgroup that has it all
+  size_t at_shared = 0;
+  if (shared.n_blk > 0) {
+    const int at = pos + i, tile = at / shared.tile_tok;
+    at_shared = parts(shared, tile, (at - tile * shared.tile_tok) * p.g + hg, n_shared);
+  }
   float M = -INFINITY, L = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  auto fold = [&](const PagedRun& r, int tile, int row) {
-    const int start = r.start + (kvh * r.n_tiles + tile) * (r.n_blk + kPagedPad);
-    const int w0 = split.owner(start), w1 = split.owner(start + r.n_blk - 1);
-    if (r.whole && w0 == w1) return false;  // written by the workgroup that has it all
-    for (int w = w0; w <= w1; ++w) {
-      const size_t at = partial_row(r, p.g, kvh, tile, w) + row;
-      const float2 ml = *(const float2*)(p.part_ml + at * 2);
-      const f32x4 a = *(const f32x4*)(p.part_acc + at * D + 4 * q4);
-      const float Mn = fmaxf(M, ml.x), Mf = Mn == -INFINITY ? 0.f : Mn;
-      const float wa = __builtin_amdgcn_exp2f(M - Mf), wb = __builtin_amdgcn_exp2f(ml.x - Mf);
-      L = L * wa + ml.y * wb;
-      acc = acc * wa + a * wb;
-      M = Mn;
+  const int n = n_own + n_shared;
+  for (int x0 = 0; x0 < n; x0 += kMergeRound) {
+    float2 ml[kMergeRound];
+    f32x4 a[kMergeRound];
+#pragma unroll
+    for (int x = 0; x < kMergeRound; ++x) {  // past the end: the last one again, with weight 0 (rounds of two for two were no quicker)
+      const int y = min(x0 + x, n - 1);
+      const size_t at = y < n_own ? at_own + (size_t)y * kSlotRows : at_shared + (size_t)(y - n_own) * kSlotRows;
+      ml[x] = *(const float2*)(p.part_ml + at * 2);
+      a[x] = *(const f32x4*)(p.part_acc + at * D + 4 * q4);
     }
-    return true;
-  };
-  if (seq.shared >= 0) {
-    const PagedRun& r = p.runs[seq.shared];
-    const int at = seq.pos + i, tile = at / r.tile_tok;
-    fold(r, tile, (at - tile * r.tile_tok) * p.g + hg);
+    const float M_old = M;
+#pragma unroll
+    for (int x = 0; x < kMergeRound; ++x) M = fmaxf(M, ml[x].x);
+    const float Mf = M == -INFINITY ? 0.f : M, alpha = __builtin_amdgcn_exp2f(M_old - Mf);
+    L *= alpha;
+    acc *= alpha;
+#pragma unroll
+    for (int x = 0; x < kMergeRound; ++x)
+      if (x0 + x < n) {
+        const float wgt = __builtin_amdgcn_exp2f(ml[x].x - Mf);
+        L += ml[x].y * wgt;
+        acc += a[x] * wgt;
+      }
   }
-  if (!fold(p.runs[seq.own], 0, i * p.g + hg)) return;
   const float inv = __builtin_amdgcn_rcpf(L);
   *(uint2*)out = to_bf16(acc * inv);
   if (p.lse && q4 == 0) p.lse[orow] = (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
@@ -679,16 +728,16 @@ extern "C" int bass_paged_verify_attention(const bass_paged_desc* d, const void*
   hipStream_t s = (hipStream_t)stream;
   const bool int8 = d->dtype == BASS_DTYPE_INT8KV;
   const dim3 grid(kPagedShares), block(64 * kPagedWaves);
-  const int64_t rows = (int64_t)d->B * d->kmax * d->Hq;
-  const dim3 merge_grid((unsigned)((rows + 1024 / d->D - 1) / (1024 / d->D)));
+  const int head_groups = (d->Hq + 1024 / d->D - 1) / (1024 / d->D);
+  const dim3 merge_grid((unsigned)(d->B * d->kmax * head_groups));
   if (d->D == 128) {
     if (int8) hipLaunchKernelGGL((paged_attn<128, true>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((paged_attn<128, false>), grid, block, 0, s, p);
-    hipLaunchKernelGGL(paged_merge<128>, merge_grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL(paged_merge<128>, merge_grid, dim3(256), 0, s, p, head_groups);
   } else {
     if (int8) hipLaunchKernelGGL((paged_attn<64, true>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((paged_attn<64, false>), grid, block, 0, s, p);
-    hipLaunchKernelGGL(paged_merge<64>, merge_grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL(paged_merge<64>, merge_grid, dim3(256), 0, s, p, head_groups);
   }
   return launch_status();
 }

@@ -10,6 +10,7 @@ constexpr int kPlanThreads2 = 1024;
 
 struct PagedPlanParams {
   int B, kmax, g, Hkv, most_tokens, n_prefixes;
+  bool int8;
   int32_t signature;
   const int32_t *ctx_len, *draft_len, *prefix_of, *prefix_len;
   PagedHeader* header;
@@ -20,33 +21,46 @@ struct PagedPlanParams {
   int32_t* status;
 };
 
-// Exclusive prefix sum over the workgroup and its total; all threads call.
-__device__ inline int scan1024(int v, int* lds, int& total) {
+// Exclusive prefix sums of four numbers at once over the workgroup, and their totals; all threads call.
+struct Four {
+  int v[4];
+};
+__device__ inline Four scan1024(Four x, Four* lds, Four& total) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  int x = v;
+  Four s = x;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int t = __shfl_up(x, o);
-    if (lane >= o) x += t;
-  }
+  for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = __shfl_up(s.v[i], o);
+      if (lane >= o) s.v[i] += t;
+    }
   __syncthreads();
-  if (lane == 63) lds[wv] = x;
+  if (lane == 63) lds[wv] = s;
   __syncthreads();
-  total = 0;
-  for (int i = 0; i < kPlanThreads2 / 64; ++i) {
-    if (i < wv) x += lds[i];
-    total += lds[i];
-  }
-  return x - v;
+  total = Four{{0, 0, 0, 0}};
+#pragma unroll
+  for (int w = 0; w < kPlanThreads2 / 64; ++w)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (w < wv) s.v[i] += lds[w].v[i];
+      total.v[i] += lds[w].v[i];
+    }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s.v[i] -= x.v[i];
+  return s;
 }
 
 __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanParams p) {
-  __shared__ int sums[kPlanThreads2 / 64];
+  __shared__ Four sums[kPlanThreads2 / 64];
   __shared__ int seq_L[kMaxPagedBatch], seq_n[kMaxPagedBatch], seq_g[kMaxPagedBatch];
   // of each prefix: least ctx_len, then common blocks; query tokens, then their first place in the list; sequences, then its run; first sequence
   __shared__ int pre_L[kMaxPagedBatch], pre_tok[kMaxPagedBatch], pre_row[kMaxPagedBatch], pre_n[kMaxPagedBatch];
   __shared__ int starts[2 * kMaxPagedBatch];
   const int tid = threadIdx.x;
+  // the first sequence of every thread, requested with the prefixes' lengths: one trip to memory
+  const bool has = tid < p.B;
+  const int my_L = has ? p.ctx_len[tid] : 0, my_n = has ? p.draft_len[tid] : 0, my_x = has && p.prefix_of ? p.prefix_of[tid] : -1;
   for (int x = tid; x < p.n_prefixes; x += kPlanThreads2) {
     pre_L[x] = p.prefix_len[x];
     pre_tok[x] = pre_n[x] = 0;
@@ -55,9 +69,9 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
   __syncthreads();
   int bad = 0;
   for (int b = tid; b < p.B; b += kPlanThreads2) {
-    int L = p.ctx_len[b], n = p.draft_len[b];
+    int L = b == tid ? my_L : p.ctx_len[b], n = b == tid ? my_n : p.draft_len[b];
     if (clamp_lengths(L, n, p.kmax, p.most_tokens)) bad = BASS_STATUS_LEN_CLAMPED;
-    int x = p.prefix_of ? p.prefix_of[b] : -1;
+    int x = b == tid ? my_x : p.prefix_of ? p.prefix_of[b] : -1;
     if (x >= p.n_prefixes) bad = BASS_STATUS_LEN_CLAMPED;
     if (x < 0 || x >= p.n_prefixes || n == 0) x = -1;
     seq_L[b] = L;
@@ -93,7 +107,6 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
         r.tile_tok = min((r.n_tok + r.n_tiles - 1) / r.n_tiles, kTileRows / p.g);
         r.n_tiles = (r.n_tok + r.tile_tok - 1) / r.tile_tok;
         r.L = -1;
-        units = r.n_tiles * p.Hkv;
       }
     } else if (x < items && seq_n[b] > 0) {
       r.row = b;
@@ -105,17 +118,21 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
       r.first = shared;
       r.n_blk = num_blocks(seq_L[b] + seq_n[b]) - shared;
       r.whole = shared == 0;
-      units = p.Hkv;
     }
-    int total;
-    const int at = n_runs + scan1024(units > 0, sums, total);
-    n_runs += total;
-    r.start = entries + scan1024(units * (r.n_blk + kPagedPad), sums, total);
-    entries += total;
-    r.row_base = rows + scan1024(units > 0 ? r.n_tok * p.g * p.Hkv : 0, sums, total);
-    rows += total;
-    const int place = listed + scan1024(list, sums, total);
-    listed += total;
+    if (r.n_tok > 0) {
+      r.heads = p.Hkv > 1 && r.n_blk <= kHeadBlocks && r.tile_tok * p.g <= kWaveRows ? kPagedWaves : 1;
+      units = r.n_tiles * ((p.Hkv + r.heads - 1) / r.heads);
+    }
+    r.cost = block_cost(r.tile_tok * p.g, r.heads, p.int8);
+    Four total;
+    const Four before = scan1024(Four{{units > 0, units * r.entries(), units > 0 ? r.n_tok * p.g * p.Hkv : 0, list}}, sums, total);
+    const int at = n_runs + before.v[0], place = listed + before.v[3];
+    r.start = entries + before.v[1];
+    r.row_base = rows + before.v[2];
+    n_runs += total.v[0];
+    entries += total.v[1];
+    rows += total.v[2];
+    listed += total.v[3];
     if (x < p.n_prefixes) {
       r.tok = place;
       pre_n[x] = units > 0 ? at : -1;
@@ -125,7 +142,7 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
       p.runs[at] = r;
       starts[at] = r.start;
     }
-    if (x >= p.n_prefixes && x < items) p.seqs[b] = PagedSeq{seq_n[b], units > 0 ? at : -1, -1, 0};
+    if (x >= p.n_prefixes && x < items) p.seqs[b] = PagedSeq{seq_n[b], 0, {0, 0}, r, PagedRun{}};
   }
   __syncthreads();
 
@@ -137,7 +154,7 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
     for (int o = pre_row[x]; o < b; ++o)
       if (seq_g[o] == x) pos += seq_n[o];
     for (int i = 0; i < seq_n[b]; ++i) p.tokens[pre_tok[x] + pos + i] = b * p.kmax + i;
-    p.seqs[b].shared = pre_n[x];
+    p.seqs[b].shared = p.runs[pre_n[x]];
     p.seqs[b].pos = pos;
   }
 
@@ -168,9 +185,8 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
       }
       s.run = lo;
       s.first = p.runs[lo];
-      const int len = s.first.n_blk + kPagedPad;
-      s.unit = (x0 - s.first.start) / len;
-      s.off = (x0 - s.first.start) % len;
+      s.unit = (x0 - s.first.start) / s.first.entries();
+      s.off = (x0 - s.first.start) % s.first.entries();
     }
     p.shares[w] = s;
   }
@@ -194,7 +210,8 @@ extern "C" int bass_paged_attention_plan(const bass_paged_desc* d, const int32_t
   const PagedLayout l = paged_layout(d);
   if (plan_bytes < l.bytes) return BASS_ERR_WORKSPACE_TOO_SMALL;
   char* at = (char*)plan;
-  PagedPlanParams p{d->B, d->kmax, d->Hq / d->Hkv, d->Hkv, d->max_pages * d->page_tokens, n_prefixes, paged_signature(d),
+  PagedPlanParams p{d->B, d->kmax, d->Hq / d->Hkv, d->Hkv, d->max_pages * d->page_tokens, n_prefixes,
+                     d->dtype == BASS_DTYPE_INT8KV, paged_signature(d),
                     ctx_len, draft_len, prefix_of, prefix_len, (PagedHeader*)at, (PagedShare*)(at + l.shares), (PagedRun*)(at + l.runs),
                     (PagedSeq*)(at + l.seqs), (int32_t*)(at + l.tokens), dev_status};
   hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads2), 0, (hipStream_t)stream, p);
