@@ -323,19 +323,6 @@ struct TileBlocks {
   __align__(16) float scales[kI8 ? 4 : 1][64];  // of K, then of V; four blocks
 };
 
-// The order in which a half turn's instructions are laid down: after each of its n matrix instructions the part of the softmax and of the LDS
-// reads that fits beside it.
-template <int n, bool kReads, bool kI8>
-__device__ inline void interleave() {
-#pragma unroll
-  for (int i = 0; i < n; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);         // matrix
-    if (kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
-    __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);         // exponential
-    __builtin_amdgcn_sched_group_barrier(0x002, kI8 ? 8 : 5, 0);  // vector
-  }
-}
-
 template <int D, bool kI8, int NT>
 __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, int wg, TileBlocks<D, kI8>& lds) {
   using G = Wide<D, kI8, NT>;
@@ -347,16 +334,18 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
   const int32_t* table = p.tables + (size_t)s.run.row * p.max_pages;
   int bad = 0;
-  auto pool_blocks = [&](int t0) {  // blocks t0 + lane, as the pool counts them
-    const int blk = s.first + min(t0 + lane, s.n - 1), at = blk / p.blocks_per_page;
-    int page = table[at];
+  // Block t0 + lane as the pool counts them (past the end: the last one), in two steps: its page's number is on its way meanwhile.
+  auto block_of_lane = [&](int t0) { return s.first + min(t0 + lane, s.n - 1); };
+  auto request = [&](int t0) { return table[block_of_lane(t0) / p.blocks_per_page]; };
+  auto arrived = [&](int page, int t0) {
     if (page < 0 || page >= p.n_pages) {
       page = 0;
       bad = 1;
     }
-    return (page * p.Hkv + s.kvh) * p.blocks_per_page + (blk - at * p.blocks_per_page);
+    const int blk = block_of_lane(t0);
+    return (page * p.Hkv + s.kvh) * p.blocks_per_page + (blk - blk / p.blocks_per_page * p.blocks_per_page);
   };
-  int now = pool_blocks(0), next = 0, base_t = 0;  // lane l: block base_t + l, base_t + 64 + l
+  int now = arrived(request(0), 0);  // lane l: block 64 w + l of window w
   // Whole rounds of 256 chunks (INT8 heads of 64: half of the threads have one).
   constexpr bool kHalf = kVec < 256;
   const int mine = kHalf ? tid & (kVec - 1) : tid;
@@ -437,27 +426,17 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   auto value = [&](int nt, int x) {
     acc[nt][x >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[x]), pf[nt][x & 1], acc[nt][x >> 1], 0, 0, 0);
   };
-  // Block t's scores as numbers, and the largest of each row.
-  float mx[NT];
-  auto peak = [&](int nt, int t) {
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      if constexpr (kI8) {
-        const f32x4 ks = *(const f32x4*)&lds.scales[t & 3][G::token(4 * y, h)] * q.row_scale[nt];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) e[nt][4 * y + i] = (float)z[nt][4 * y + i] * ks[i];
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) e[nt][4 * y + i] = z[nt][4 * y + i];
-      }
-    }
-    float x = e[nt][0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) x = fmaxf(x, e[nt][i]);
-    mx[nt] = F::row_max(x);
+  // Softmax of a tile of rows, element by element (16 of a lane), so that it can be laid between matrix instructions.
+  float mx[NT], sum[NT], m_use[NT], arg[NT][16];
+  // Score i of block t as a number.  INT8: times the scales of token and row, multiplied first.
+  auto take = [&](int nt, int i, int t) {
+    if constexpr (kI8) e[nt][i] = (float)z[nt][i] * (lds.scales[t & 3][G::token(i, h)] * q.row_scale[nt]);
+    else e[nt][i] = z[nt][i];
+    mx[nt] = i == 0 ? e[nt][0] : fmaxf(mx[nt], e[nt][i]);
   };
   // The row's reference maximum moves when a block exceeds it by more than kMaxSlack.
   auto settle = [&](int nt) {
+    mx[nt] = F::row_max(mx[nt]);
     const bool grow = (mx[nt] - m[nt]) * factor > kMaxSlack;  // from -inf: infinite
     if (__any(grow)) {
       const float m_new = grow ? mx[nt] : m[nt];
@@ -467,63 +446,79 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
       for (int a = 0; a < F::kAcc; ++a) acc[nt][a] *= alpha;
       m[nt] = m_new;
     }
+    m_use[nt] = m[nt] == -INFINITY ? 0.f : m[nt];  // no score above -inf yet
+    sum[nt] = 0.f;
   };
-  auto probabilities = [&](int nt, int t, bool counts) {
-    const float m_use = m[nt] == -INFINITY ? 0.f : m[nt];  // no score above -inf yet
-    float sum = 0.f;
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      f32x4 vs = {1.f, 1.f, 1.f, 1.f};
-      if constexpr (kI8) vs = *(const f32x4*)&lds.scales[t & 3][32 + G::token(4 * y, h)];
-#pragma unroll
-      for (int i = 4 * y; i < 4 * y + 4; ++i) {
-        const float x = __builtin_amdgcn_exp2f(kI8 ? e[nt][i] - m_use : (e[nt][i] - m_use) * factor);
-        sum += x;
-        pf[nt][i >> 3][i & 7] = (__bf16)(kI8 ? x * vs[i & 3] : x);
+  // Probability i in three steps, one behind the other: argument, exponential, sum and operand.
+  auto soft = [&](int nt, int i, int t) {
+    if (i < 16) arg[nt][i] = kI8 ? e[nt][i] - m_use[nt] : (e[nt][i] - m_use[nt]) * factor;
+    if (i >= 1 && i < 17) e[nt][i - 1] = __builtin_amdgcn_exp2f(arg[nt][i - 1]);
+    if (i >= 2 && i < 18) {
+      const int j = i - 2;
+      sum[nt] += e[nt][j];
+      if (j & 1) {
+        if constexpr (kI8) {
+          pf[nt][j >> 3][(j & 7) - 1] = (__bf16)(e[nt][j - 1] * lds.scales[t & 3][32 + G::token(j - 1, h)]);
+          pf[nt][j >> 3][j & 7] = (__bf16)(e[nt][j] * lds.scales[t & 3][32 + G::token(j, h)]);
+        } else {
+          pf[nt][j >> 3][(j & 7) - 1] = (__bf16)e[nt][j - 1];
+          pf[nt][j >> 3][j & 7] = (__bf16)e[nt][j];
+        }
       }
     }
-    l[nt] += counts ? sum : 0.f;
-    // here, not where they are needed: in front of the branch of settle()
-    asm volatile("" : "+v"(pf[nt][0]), "+v"(pf[nt][1]), "+v"(l[nt]));
+  };
+  auto finish = [&](int nt, bool counts) {
+    l[nt] += counts ? sum[nt] : 0.f;
+    asm volatile("" : "+v"(pf[nt][0]), "+v"(pf[nt][1]), "+v"(l[nt]));  // in front of the branch of settle(), not where it is needed
   };
   // Two tiles of rows go through the blocks half a block apart, so that the matrix instructions of one stand beside the softmax of the
   // other: turn t is  [scores of A, block t + 1; values of A, block t | probabilities of B, block t], then
   // [scores of B, block t + 1; values of B, block t | probabilities of A, block t + 1].  Operands are read from LDS in the second half, each as soon
   // as its last use is past.  The last turn's scores are of the last block again, and their probabilities are not counted.
-  int v_blk = 0;  // block t + 3
+  // A wavefront has its SIMD for itself: what is to run beside a matrix instruction has to stand right behind it, and the compiler, left to
+  // itself, gathers the matrix instructions and lets the rest wait (200 instead of .. us).
+  constexpr int kHalf16 = kSteps + kFrags;  // matrix instructions of a half turn
+  int v_blk = 0;                            // block t + 3
+  auto half_turn = [&](auto tile_m, auto tile_s, int t, int t_soft, bool counts, auto beside) {
+    constexpr int nm = decltype(tile_m)::value, ns = decltype(tile_s)::value;
+#pragma unroll
+    for (int x = 0; x < kHalf16; ++x) {
+      if (x < kSteps) score(nm, x);
+      else value(nm, x - kSteps);
+#pragma unroll
+      for (int i = x * 18 / kHalf16; i < (x + 1) * 18 / kHalf16; ++i) soft(ns, i, t_soft);
+      if (x > kSteps) {
+        constexpr int n = kFrags - 1;
+        const int y = x - kSteps - 1;
+#pragma unroll
+        for (int i = y * 16 / n; i < (y + 1) * 16 / n; ++i) take(nm, i, t + 1);
+      }
+      beside(x);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    finish(ns, counts);
+    settle(nm);
+  };
   auto turn = [&](int t, Stage& k_stage, Stage& v_stage) {
     const bool more = t + 1 < s.n;
     const int k_blk = block_of(t + 4);
-    commit_k(k_stage, t + 2);
-    commit_v(v_stage, t + 1);
-    fetch_k(k_stage, k_blk);
-    fetch(v_stage, p.Vp, v_blk);
-    v_blk = k_blk;
     if constexpr (NT == 2) {
-#pragma unroll
-      for (int x = 0; x < kSteps; ++x) score(0, x);
-#pragma unroll
-      for (int x = 0; x < kFrags; ++x) value(0, x);
-      probabilities(1, t, true);
-      peak(0, t + 1);
-      interleave<kSteps + kFrags, false, kI8>();
-      settle(0);
+      half_turn(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{}, t, t, true, [&](int x) {
+        if (x == 1) commit_k(k_stage, t + 2);
+        if (x == 2) commit_v(v_stage, t + 1);
+        if (x == 4) fetch_k(k_stage, k_blk);
+        if (x == 5) fetch(v_stage, p.Vp, v_blk);
+      });
       __syncthreads();
-#pragma unroll
-      for (int x = 0; x < kSteps; ++x) {
-        score(1, x);
-        read_k(x, t + 2);
-      }
-#pragma unroll
-      for (int x = 0; x < kFrags; ++x) {
-        value(1, x);
-        read_v(x, t + 1);
-      }
-      probabilities(0, t + 1, more);
-      peak(1, t + 1);
-      interleave<kSteps + kFrags, true, kI8>();
-      settle(1);
+      half_turn(std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{}, t, t + 1, more, [&](int x) {
+        if (x < kSteps) read_k(x, t + 2);
+        else read_v(x - kSteps, t + 1);
+      });
     } else {
+      commit_k(k_stage, t + 2);
+      commit_v(v_stage, t + 1);
+      fetch_k(k_stage, k_blk);
+      fetch(v_stage, p.Vp, v_blk);
       __syncthreads();
 #pragma unroll
       for (int x = 0; x < kSteps; ++x) {
@@ -535,17 +530,21 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
         value(0, x);
         read_v(x, t + 1);
       }
-      peak(0, t + 1);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) take(0, i, t + 1);
       settle(0);
-      probabilities(0, t + 1, more);
+#pragma unroll
+      for (int i = 0; i < 18; ++i) soft(0, i, t + 1);
+      finish(0, more);
     }
+    v_blk = k_blk;
   };
   commit_k(k_even, 0);
   commit_k(k_odd, 1);
   commit_v(v_even, 0);
-  fetch_k(k_even, block_of(2));
-  fetch_k(k_odd, block_of(3));
+  fetch_k(k_even, block_of(2));  // in the order of the turns: the wait counts of the loop's entry and of its end are the same
   fetch(v_even, p.Vp, block_of(1));
+  fetch_k(k_odd, block_of(3));
   fetch(v_odd, p.Vp, block_of(2));
   v_blk = block_of(3);
   __syncthreads();
@@ -560,29 +559,33 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   for (int x = 0; x < kFrags; ++x) read_v(x, 0);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    peak(nt, 0);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) take(nt, i, 0);
     settle(nt);
   }
-  probabilities(0, 0, true);
+#pragma unroll
+  for (int i = 0; i < 18; ++i) soft(0, i, 0);
+  finish(0, true);
   __syncthreads();  // before the first turn writes over block 0
-  for (int t = 0; t < s.n; t += 2) {
-    if (t + 4 - base_t == 64) {
-      base_t += 64;
-      now = next;
+  // Windows of 64 blocks: turn t asks for block t + 4.  The inner loop has no loads but those of the stages, so that its wait counts are exact.
+  for (int t = 0, end = 60;; end += 64) {
+    const int page = request(end + 4);
+    for (; t < min(end, s.n); t += 2) {
+      turn(t, k_even, v_even);
+      if (t + 1 >= s.n) break;
+      turn(t + 1, k_odd, v_odd);
     }
-    if (t + 4 - base_t == 32) next = pool_blocks(base_t + 64);
-    turn(t, k_even, v_even);
-    if (t + 1 >= s.n) break;
-    turn(t + 1, k_odd, v_odd);
+    if (end >= s.n) break;
+    now = arrived(page, end + 4);
   }
   if (bad && p.status) atomicOr(p.status, BASS_STATUS_PAGE_CLAMPED);
   const size_t base = partial_row(s.run, p.g, s.kvh, s.tile, wg);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int row = row0 + 32 * nt + c;
-    const float sum = F::row_sum(l[nt]);
+    const float all = F::row_sum(l[nt]);
     if (row < rows) {
-      if (h == 0) *(float2*)(p.part_ml + (base + row) * 2) = make_float2(m[nt] * factor, sum);
+      if (h == 0) *(float2*)(p.part_ml + (base + row) * 2) = make_float2(m[nt] * factor, all);
 #pragma unroll
       for (int a = 0; a < F::kAcc; ++a)
 #pragma unroll

@@ -151,8 +151,8 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
     const int x = seq_g[b];
     if (x < 0 || pre_n[x] < 0) continue;
     int pos = 0;
-    for (int o = pre_row[x]; o < b; ++o)
-      if (seq_g[o] == x) pos += seq_n[o];
+#pragma unroll 8
+    for (int o = pre_row[x]; o < b; ++o) pos += seq_g[o] == x ? seq_n[o] : 0;
     for (int i = 0; i < seq_n[b]; ++i) p.tokens[pre_tok[x] + pos + i] = b * p.kmax + i;
     p.seqs[b].shared = p.runs[pre_n[x]];
     p.seqs[b].pos = pos;
