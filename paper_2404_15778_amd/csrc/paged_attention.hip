@@ -45,10 +45,10 @@ struct PagedSegment {
 
 __device__ inline PagedRun uniform_run(const PagedRun* at) {
   const i32x4 a = ((const i32x4*)at)[0], b = ((const i32x4*)at)[1], c = ((const i32x4*)at)[2];
-  const int heads = ((const int*)at)[12];
+  const i32x4 d = ((const i32x4*)at)[3];
   return PagedRun{uniform(a[0]), uniform(a[1]), uniform(a[2]), uniform(a[3]), uniform(b[0]), uniform(b[1]), uniform(b[2]), uniform(b[3]),
                   uniform(c[0]), uniform(c[1]), uniform(c[2]), uniform(c[3]),
-                  uniform(heads), {0, 0, 0}};
+                  uniform(d[0]), uniform(d[1]), {0, 0}};
 }
 
 __device__ inline PagedSegment paged_segment(const PagedRun& r, int unit, int off, int entries) {
@@ -473,8 +473,8 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   };
   // Two tiles of rows go through the blocks half a block apart, so that the matrix instructions of one stand beside the softmax of the
   // other: turn t is  [scores of A, block t + 1; values of A, block t | probabilities of B, block t], then
-  // [scores of B, block t + 1; values of B, block t | probabilities of A, block t + 1].  Operands are read from LDS in the second half, each as soon
-  // as its last use is past.  The last turn's scores are of the last block again, and their probabilities are not counted.
+  // [scores of B, block t + 1; values of B, block t | probabilities of A, block t + 1].  Operands are read from LDS eight matrix instructions ahead, V in
+  // the first half and K in the second, behind their last use.  The last turn's scores are of the last block again, and their probabilities are not counted.
   // A wavefront has its SIMD for itself: what is to run beside a matrix instruction has to stand right behind it, and the compiler, left to
   // itself, gathers the matrix instructions and lets the rest wait (200 instead of .. us).
   constexpr int kHalf16 = kSteps + kFrags;  // matrix instructions of a half turn
@@ -504,6 +504,7 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
     const int k_blk = block_of(t + 4);
     if constexpr (NT == 2) {
       half_turn(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{}, t, t, true, [&](int x) {
+        if (x < kFrags) read_v(x, t);
         if (x == 1) commit_k(k_stage, t + 2);
         if (x == 2) commit_v(v_stage, t + 1);
         if (x == 4) fetch_k(k_stage, k_blk);
@@ -512,7 +513,6 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
       __syncthreads();
       half_turn(std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{}, t, t + 1, more, [&](int x) {
         if (x < kSteps) read_k(x, t + 2);
-        else read_v(x - kSteps, t + 1);
       });
     } else {
       commit_k(k_stage, t + 2);
@@ -555,8 +555,10 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
     for (int nt = 0; nt < NT; ++nt) score(nt, x);
     read_k(x, 1);
   }
+  if constexpr (NT == 1) {
 #pragma unroll
-  for (int x = 0; x < kFrags; ++x) read_v(x, 0);
+    for (int x = 0; x < kFrags; ++x) read_v(x, 0);
+  }
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -567,17 +569,19 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   for (int i = 0; i < 18; ++i) soft(0, i, 0);
   finish(0, true);
   __syncthreads();  // before the first turn writes over block 0
-  // Windows of 64 blocks: turn t asks for block t + 4.  The inner loop has no loads but those of the stages, so that its wait counts are exact.
-  for (int t = 0, end = 60;; end += 64) {
+  // Windows of 64 blocks: turn t asks for block t + 4.  The inner loop has no loads but those of the stages and no way out between its two
+  // turns, so that its wait counts are exact.
+  int t = 0;
+  for (int end = 60;; end += 64) {
     const int page = request(end + 4);
-    for (; t < min(end, s.n); t += 2) {
+    for (const int stop = min(end, s.n) - 1; t < stop; t += 2) {
       turn(t, k_even, v_even);
-      if (t + 1 >= s.n) break;
       turn(t + 1, k_odd, v_odd);
     }
     if (end >= s.n) break;
     now = arrived(page, end + 4);
   }
+  if (t < s.n) turn(t, k_even, v_even);
   if (bad && p.status) atomicOr(p.status, BASS_STATUS_PAGE_CLAMPED);
   const size_t base = partial_row(s.run, p.g, s.kvh, s.tile, wg);
 #pragma unroll

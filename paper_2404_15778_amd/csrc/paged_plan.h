@@ -4,8 +4,8 @@
 // all of them, or the rest of one sequence, with its own.  A run's query tokens are cut into tiles, and every (kv head, tile) of a run is a
 // unit of the run's n_blk blocks; in short runs, where the end of a unit would cost its workgroup more than the blocks, four kv heads are one
 // unit, a wavefront each.  All units are laid end to end and the list is divided evenly over the workgroups.  An entry of the list is a
-// stretch of time, not of blocks: a block takes `cost` entries, by what its workgroup does with it, and a unit ends with kPagedPad entries more (states
-// merged, a partial result stored).  A block belongs to the workgroup that has its first entry.  Units of a shared run are in the order of
+// stretch of time, not of blocks: a block takes `cost` entries, by what its workgroup does with it, and a unit ends with `pad` entries more (states
+// merged, a partial result stored, the next one's first blocks waited for).  A block belongs to the workgroup that has its first entry.  Units of a shared run are in the order of
 // the kv heads: the tiles of a kv head read the same blocks, on the same XCD at about the same time.
 #pragma once
 #include "paged.h"
@@ -14,13 +14,14 @@ namespace bass {
 
 constexpr int kPagedWaves = 4;      // wavefronts of a workgroup
 constexpr int kPagedShares = 256;   // workgroups of the attention launch: one per compute unit
-// Entries of a block.  Up to 64 rows (four blocks at a time, a wavefront each): 0.5 us; tiles (a block at a time, all wavefronts): 128 rows and
-// 256 rows over bf16 / INT8 pages.
-constexpr int kCostRows = 2, kCostTile1 = 3, kCostTile2 = 5, kCostTile1Int8 = 5, kCostTile2Int8 = 8;
-constexpr int kPagedPad = 12;
+// An entry is 1/8 us.  Of a block: up to 32 and 64 rows (four blocks at a time, a wavefront each); tiles of 128 and 256 rows (a block at a time, all
+// wavefronts) over bf16 and INT8 pages.  Of the end of a unit, with the beginning of the next: by a wavefront per head, by all four, and of a tile.
+constexpr int kCostRows1 = 4, kCostRows2 = 6, kCostTile1 = 6, kCostTile2 = 8, kCostTile1Int8 = 9, kCostTile2Int8 = 13;
+constexpr int kPadHeads = 32, kPadRows = 40, kPadTile = 76;
+constexpr int kTileStart = 48;  // a workgroup that begins with a tile loses so much more than one that begins with few rows (see tile_cost)
 // Runs of at most so many blocks give each wavefront a kv head: nothing is merged, but a workgroup has four partial results.
 constexpr int kHeadBlocks = 48;
-constexpr int kLeastEntries = 16;   // of a workgroup, as long as there are fewer workgroups than kPagedShares; at least the largest cost
+constexpr int kLeastEntries = 40;   // of a workgroup, as long as there are fewer workgroups than kPagedShares; at least the largest cost
 constexpr int kTileRows = 256;      // most query rows of a tile
 constexpr int kSlotRows = kTileRows;  // rows between the partial results of two workgroups (see partial_row)
 constexpr int kLeastShared = 4;     // a common prefix of fewer blocks is left to the sequences themselves
@@ -38,17 +39,22 @@ struct PagedRun {
   int32_t row_base;  // partial rows before this run
   int32_t whole;     // 1: the sequence has no shared part, so a unit that is not cut is the final result
   int32_t cost;      // entries of a block
+  int32_t pad;       // entries of the unit's end
   int32_t heads;     // kv heads of a unit: 1, or one for each wavefront
-  int32_t reserved[3];
-  BASS_HD int entries() const { return n_blk * cost + kPagedPad; }                          // of a unit
+  int32_t reserved[2];
+  BASS_HD int entries() const { return n_blk * cost + pad; }                                // of a unit
   BASS_HD int block_at(int entry) const { return imin((entry + cost - 1) / cost, n_blk); }  // first block that starts at `entry` or behind it
 };
 
-// A tile's kernel and what a block costs it.
-constexpr int kWaveRows = 64;  // up to so many rows every wavefront has all of them
+constexpr int kWaveRows = 64;  // up to so many rows of a tile every wavefront has all of them
 BASS_HD inline int block_cost(int tile_rows, int heads, bool int8) {
-  return tile_rows <= kWaveRows ? kCostRows * heads : tile_rows <= kTileRows / 2 ? (int8 ? kCostTile1Int8 : kCostTile1) : int8 ? kCostTile2Int8 : kCostTile2;
+  if (tile_rows <= kWaveRows) return (tile_rows <= kWaveRows / 2 ? kCostRows1 : kCostRows2) * heads;
+  return tile_rows <= kTileRows / 2 ? (int8 ? kCostTile1Int8 : kCostTile1) : int8 ? kCostTile2Int8 : kCostTile2;
 }
+BASS_HD inline int unit_pad(int tile_rows, int heads) { return tile_rows > kWaveRows ? kPadTile : heads > 1 ? kPadHeads : kPadRows; }
+// Every workgroup pays for a beginning, those with tiles more; in short lists that is much of their time, so that a tile's block counts for more there.
+// per: entries of a workgroup by the plain costs.
+BASS_HD inline int tile_cost(int cost, int per) { return (int)((int64_t)cost * per / imax(per - kTileStart, per / 3 + 1)) + 1; }
 
 struct PagedHeader {
   int32_t signature, n_runs, total, per, rem, used;
@@ -114,7 +120,7 @@ inline int check_paged_attention(const bass_paged_desc* d) {
   if (d->B > kMaxPagedBatch || (int64_t)d->kmax * (d->Hq / d->Hkv) > 64) return BASS_ERR_UNSUPPORTED;
   // the list counts in 32 bits: every sequence's blocks, and at most as many again of shared runs
   const int64_t blocks = (int64_t)d->max_pages * (d->page_tokens / kBlockTokens);
-  if (((kCostRows + kCostTile2Int8) * blocks + 2 * kPagedPad) * d->B * d->Hkv >= (1ll << 31) || 2 * (int64_t)d->B * d->kmax * d->Hq >= (1ll << 31)) return BASS_ERR_UNSUPPORTED;
+  if (((kCostRows2 + 3 * kCostTile2Int8) * blocks + kPadRows + kPadTile) * d->B * d->Hkv >= (1ll << 31) || 2 * (int64_t)d->B * d->kmax * d->Hq >= (1ll << 31)) return BASS_ERR_UNSUPPORTED;
   return BASS_OK;
 }
 

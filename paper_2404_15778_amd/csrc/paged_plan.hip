@@ -92,57 +92,65 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
   __syncthreads();
 
   // Runs: item x < n_prefixes is a prefix, the others are the sequences.
-  int n_runs = 0, entries = 0, rows = 0, listed = 0;
+  // Two passes where there are prefixes: the first finds how long the list is by the plain costs.
+  int n_runs = 0, entries = 0, rows = 0, listed = 0, per = 0;
   const int items = p.n_prefixes + p.B;
-  for (int x0 = 0; x0 < items; x0 += kPlanThreads2) {
-    const int x = x0 + tid, b = x - p.n_prefixes;
-    PagedRun r{};
-    int units = 0, list = 0;
-    if (x < p.n_prefixes) {
-      r.n_blk = pre_L[x];
-      if (r.n_blk > 0) {
-        r.row = pre_row[x];
-        r.n_tok = list = pre_tok[x];
-        r.n_tiles = (r.n_tok * p.g + kTileRows - 1) / kTileRows;
-        r.tile_tok = min((r.n_tok + r.n_tiles - 1) / r.n_tiles, kTileRows / p.g);
-        r.n_tiles = (r.n_tok + r.tile_tok - 1) / r.tile_tok;
-        r.L = -1;
+  for (int pass = p.n_prefixes > 0 ? 0 : 1; pass < 2; ++pass) {
+    per = min(entries / kPagedShares, 1 << 20);
+    n_runs = entries = rows = listed = 0;
+    for (int x0 = 0; x0 < items; x0 += kPlanThreads2) {
+      const int x = x0 + tid, b = x - p.n_prefixes;
+      PagedRun r{};
+      int units = 0, list = 0;
+      if (x < p.n_prefixes) {
+        r.n_blk = pre_L[x];
+        if (r.n_blk > 0) {
+          r.row = pre_row[x];
+          r.n_tok = list = pre_tok[x];
+          r.n_tiles = (r.n_tok * p.g + kTileRows - 1) / kTileRows;
+          r.tile_tok = min((r.n_tok + r.n_tiles - 1) / r.n_tiles, kTileRows / p.g);
+          r.n_tiles = (r.n_tok + r.tile_tok - 1) / r.tile_tok;
+          r.L = -1;
+        }
+      } else if (x < items && seq_n[b] > 0) {
+        r.row = b;
+        r.tok = b * p.kmax;
+        r.n_tok = r.tile_tok = seq_n[b];
+        r.n_tiles = 1;
+        r.L = seq_L[b];
+        const int shared = seq_g[b] >= 0 ? pre_L[seq_g[b]] : 0;
+        r.first = shared;
+        r.n_blk = num_blocks(seq_L[b] + seq_n[b]) - shared;
+        r.whole = shared == 0;
       }
-    } else if (x < items && seq_n[b] > 0) {
-      r.row = b;
-      r.tok = b * p.kmax;
-      r.n_tok = r.tile_tok = seq_n[b];
-      r.n_tiles = 1;
-      r.L = seq_L[b];
-      const int shared = seq_g[b] >= 0 ? pre_L[seq_g[b]] : 0;
-      r.first = shared;
-      r.n_blk = num_blocks(seq_L[b] + seq_n[b]) - shared;
-      r.whole = shared == 0;
+      if (r.n_tok > 0) {
+        r.heads = p.Hkv > 1 && r.n_blk <= kHeadBlocks && r.tile_tok * p.g <= kWaveRows ? kPagedWaves : 1;
+        units = r.n_tiles * ((p.Hkv + r.heads - 1) / r.heads);
+      }
+      r.cost = block_cost(r.tile_tok * p.g, r.heads, p.int8);
+      if (pass == 1 && r.tile_tok * p.g > kWaveRows) r.cost = tile_cost(r.cost, per);
+      r.pad = unit_pad(r.tile_tok * p.g, r.heads);
+      Four total;
+      const Four before = scan1024(Four{{units > 0, units * r.entries(), units > 0 ? r.n_tok * p.g * p.Hkv : 0, list}}, sums, total);
+      const int at = n_runs + before.v[0], place = listed + before.v[3];
+      r.start = entries + before.v[1];
+      r.row_base = rows + before.v[2];
+      n_runs += total.v[0];
+      entries += total.v[1];
+      rows += total.v[2];
+      listed += total.v[3];
+      if (pass == 0) continue;
+      if (x < p.n_prefixes) {
+        r.tok = place;
+        pre_n[x] = units > 0 ? at : -1;
+        pre_tok[x] = place;
+      }
+      if (units > 0) {
+        p.runs[at] = r;
+        starts[at] = r.start;
+      }
+      if (x >= p.n_prefixes && x < items) p.seqs[b] = PagedSeq{seq_n[b], 0, {0, 0}, r, PagedRun{}};
     }
-    if (r.n_tok > 0) {
-      r.heads = p.Hkv > 1 && r.n_blk <= kHeadBlocks && r.tile_tok * p.g <= kWaveRows ? kPagedWaves : 1;
-      units = r.n_tiles * ((p.Hkv + r.heads - 1) / r.heads);
-    }
-    r.cost = block_cost(r.tile_tok * p.g, r.heads, p.int8);
-    Four total;
-    const Four before = scan1024(Four{{units > 0, units * r.entries(), units > 0 ? r.n_tok * p.g * p.Hkv : 0, list}}, sums, total);
-    const int at = n_runs + before.v[0], place = listed + before.v[3];
-    r.start = entries + before.v[1];
-    r.row_base = rows + before.v[2];
-    n_runs += total.v[0];
-    entries += total.v[1];
-    rows += total.v[2];
-    listed += total.v[3];
-    if (x < p.n_prefixes) {
-      r.tok = place;
-      pre_n[x] = units > 0 ? at : -1;
-      pre_tok[x] = place;
-    }
-    if (units > 0) {
-      p.runs[at] = r;
-      starts[at] = r.start;
-    }
-    if (x >= p.n_prefixes && x < items) p.seqs[b] = PagedSeq{seq_n[b], 0, {0, 0}, r, PagedRun{}};
   }
   __syncthreads();
 
