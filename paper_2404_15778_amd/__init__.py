@@ -9,6 +9,7 @@ see build.py) importing works but every call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -521,16 +522,33 @@ def bass_paged_attention_workspace_bytes(desc: PagedDesc) -> int:
     return int(lib().bass_paged_attention_workspace_bytes(ctypes.byref(desc)))
 
 
+class _PagedSizes:
+    """Tensor shapes and buffer sizes that follow from a descriptor's values."""
+
+    def __init__(self, raw):
+        d = PagedDesc.from_buffer_copy(raw)
+        self.batch, self.slots, self.rows = (d.B,), (d.B, d.kmax), (d.B, d.kmax, d.Hkv, d.D)
+        self.tables, self.q, self.lse = (d.B, d.max_pages), (d.B, d.kmax, d.Hq, d.D), (d.B, d.kmax, d.Hq)
+        self.pool, self.plan = bass_page_pool_bytes(d), bass_paged_attention_plan_bytes(d)
+
+
+# Asking the library for sizes and reading a descriptor's fields one by one is 2 us of a call of 7; the sizes depend on its values alone.
+_paged_sizes = functools.lru_cache(maxsize=512)(_PagedSizes)
+
+
+def _sizes_of(desc):
+    if not isinstance(desc, PagedDesc):
+        raise ValueError("desc must be a PagedDesc (make_paged_desc)")
+    return _paged_sizes(bytes(desc))
+
+
 def _bytes_of(t, need, name):
     """Device pointer of a contiguous GPU tensor of any type that holds at least `need` bytes."""
-    if _nbytes(t, name) < need:
-        raise ValueError(f"{name} holds {_nbytes(t, name)} bytes, {need} are needed")
+    if t is None or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous GPU tensor")
+    if t.nbytes < need:
+        raise ValueError(f"{name} holds {t.nbytes} bytes, {need} are needed")
     return t.data_ptr()
-
-
-def _pool_ptrs(Kpool, Vpool, desc):
-    need = lib().bass_page_pool_bytes(ctypes.byref(desc))
-    return _bytes_of(Kpool, need, "Kpool"), _bytes_of(Vpool, need, "Vpool")
 
 
 def _launch_on(stream, anchor, *others):
@@ -540,9 +558,12 @@ def _launch_on(stream, anchor, *others):
     for t in others:
         if t is not None and t.get_device() != index:
             raise ValueError("all tensors of a call must live on the same GPU")
-    if index != _torch()._C._cuda_getDevice():
+    c = _torch()._C
+    if index != c._cuda_getDevice():
         raise ValueError("the tensors must live on the current GPU (torch.cuda.device)")
-    return _stream(stream)
+    if stream is None:
+        return c._cuda_getCurrentRawStream(index)
+    return getattr(stream, "cuda_stream", stream)
 
 
 def bass_page_tables(length, held, tables, refs, page_tokens, workspace, share_from=None, share_len=None, ctx_len=None, n_new=None, slots=None,
@@ -563,68 +584,63 @@ def bass_page_tables(length, held, tables, refs, page_tokens, workspace, share_f
             _dev(slots, "slots", i32, (rows, kmax), optional=True))
     ws = _bytes_of(workspace, 0, "workspace")
     _check(lib().bass_page_tables(
-        rows, max_pages, int(page_tokens), n_pages, *args, ws, _nbytes(workspace, "workspace"),
-        _dev(dev_status, "dev_status", i32, optional=True),
+        rows, max_pages, int(page_tokens), n_pages, *args, ws, workspace.nbytes, _dev(dev_status, "dev_status", i32, optional=True),
         _launch_on(stream, tables, length, share_from, share_len, held, refs, ctx_len, n_new, slots, workspace, dev_status)), "bass_page_tables")
 
 
 def bass_paged_append(desc, Kpool, Vpool, K_new, V_new, slots, dev_status=None, stream=None):
-    torch = _torch()
-    rows = (desc.B, desc.kmax, desc.Hkv, desc.D)
+    torch, z = _torch(), _sizes_of(desc)
+    bf16, i32 = torch.bfloat16, torch.int32
     _check(lib().bass_paged_append(
-        ctypes.byref(desc), *_pool_ptrs(Kpool, Vpool, desc), _dev(K_new, "K_new", torch.bfloat16, rows), _dev(V_new, "V_new", torch.bfloat16, rows),
-        _dev(slots, "slots", torch.int32, rows[:2]), _dev(dev_status, "dev_status", torch.int32, optional=True),
+        ctypes.byref(desc), _bytes_of(Kpool, z.pool, "Kpool"), _bytes_of(Vpool, z.pool, "Vpool"), _dev(K_new, "K_new", bf16, z.rows),
+        _dev(V_new, "V_new", bf16, z.rows), _dev(slots, "slots", i32, z.slots), _dev(dev_status, "dev_status", i32, optional=True),
         _launch_on(stream, Kpool, Vpool, K_new, V_new, slots, dev_status)), "bass_paged_append")
 
 
-def _gather_args(desc, tables, start, n):
-    i32 = _torch().int32
-    return (_dev(tables, "tables", i32, (desc.B, desc.max_pages)), _dev(start, "start", i32, (desc.B,)), _dev(n, "n", i32, (desc.B,)))
-
-
 def bass_paged_gather(desc, Kpool, Vpool, K_out, V_out, tables, start, n, dev_status=None, stream=None):
-    torch = _torch()
-    rows = (desc.B, desc.kmax, desc.Hkv, desc.D)
+    torch, z = _torch(), _sizes_of(desc)
+    bf16, i32 = torch.bfloat16, torch.int32
     _check(lib().bass_paged_gather(
-        ctypes.byref(desc), *_pool_ptrs(Kpool, Vpool, desc), _dev(K_out, "K_out", torch.bfloat16, rows), _dev(V_out, "V_out", torch.bfloat16, rows),
-        *_gather_args(desc, tables, start, n), _dev(dev_status, "dev_status", torch.int32, optional=True),
+        ctypes.byref(desc), _bytes_of(Kpool, z.pool, "Kpool"), _bytes_of(Vpool, z.pool, "Vpool"), _dev(K_out, "K_out", bf16, z.rows),
+        _dev(V_out, "V_out", bf16, z.rows), _dev(tables, "tables", i32, z.tables), _dev(start, "start", i32, z.batch), _dev(n, "n", i32, z.batch),
+        _dev(dev_status, "dev_status", i32, optional=True),
         _launch_on(stream, Kpool, Vpool, K_out, V_out, tables, start, n, dev_status)), "bass_paged_gather")
 
 
 def bass_paged_gather_int8(desc, Kpool, Vpool, K_codes, V_codes, K_scales, V_scales, tables, start, n, dev_status=None, stream=None):
-    torch = _torch()
-    rows = (desc.B, desc.kmax, desc.Hkv, desc.D)
+    torch, z = _torch(), _sizes_of(desc)
+    i8, f32, i32 = torch.int8, torch.float32, torch.int32
     _check(lib().bass_paged_gather_int8(
-        ctypes.byref(desc), *_pool_ptrs(Kpool, Vpool, desc), _dev(K_codes, "K_codes", torch.int8, rows), _dev(V_codes, "V_codes", torch.int8, rows),
-        _dev(K_scales, "K_scales", torch.float32, rows[:3]), _dev(V_scales, "V_scales", torch.float32, rows[:3]),
-        *_gather_args(desc, tables, start, n), _dev(dev_status, "dev_status", torch.int32, optional=True),
+        ctypes.byref(desc), _bytes_of(Kpool, z.pool, "Kpool"), _bytes_of(Vpool, z.pool, "Vpool"), _dev(K_codes, "K_codes", i8, z.rows),
+        _dev(V_codes, "V_codes", i8, z.rows), _dev(K_scales, "K_scales", f32, z.rows[:3]), _dev(V_scales, "V_scales", f32, z.rows[:3]),
+        _dev(tables, "tables", i32, z.tables), _dev(start, "start", i32, z.batch), _dev(n, "n", i32, z.batch),
+        _dev(dev_status, "dev_status", i32, optional=True),
         _launch_on(stream, Kpool, Vpool, K_codes, V_codes, K_scales, V_scales, tables, start, n, dev_status)), "bass_paged_gather_int8")
 
 
 def bass_paged_attention_plan(desc, ctx_len, draft_len, prefix_of, prefix_len, plan, dev_status=None, stream=None):
     """prefix_of [B] (negative: none) and prefix_len [n_prefixes], or None for both: nothing is shared."""
-    i32 = _torch().int32
+    i32, z = _torch().int32, _sizes_of(desc)
     if (prefix_of is None) != (prefix_len is None):
         raise ValueError("prefix_of and prefix_len go together")
     if prefix_len is not None and (prefix_len.dim() != 1 or prefix_len.shape[0] == 0):
         raise ValueError("prefix_len must be [n_prefixes]")
-    one, need = (desc.B,), bass_paged_attention_plan_bytes(desc)
     _check(lib().bass_paged_attention_plan(
-        ctypes.byref(desc), _dev(ctx_len, "ctx_len", i32, one), _dev(draft_len, "draft_len", i32, one),
-        _dev(prefix_of, "prefix_of", i32, one, optional=True), _dev(prefix_len, "prefix_len", i32, optional=True),
-        0 if prefix_len is None else prefix_len.shape[0], _bytes_of(plan, need, "plan"), _nbytes(plan, "plan"),
+        ctypes.byref(desc), _dev(ctx_len, "ctx_len", i32, z.batch), _dev(draft_len, "draft_len", i32, z.batch),
+        _dev(prefix_of, "prefix_of", i32, z.batch, optional=True), _dev(prefix_len, "prefix_len", i32, optional=True),
+        0 if prefix_len is None else prefix_len.shape[0], _bytes_of(plan, z.plan, "plan"), plan.nbytes,
         _dev(dev_status, "dev_status", i32, optional=True),
         _launch_on(stream, plan, ctx_len, draft_len, prefix_of, prefix_len, dev_status)), "bass_paged_attention_plan")
 
 
 def bass_paged_verify_attention(desc, Q, Kpool, Vpool, tables, plan, O, lse, workspace, dev_status=None, stream=None):
-    torch = _torch()
-    q = (desc.B, desc.kmax, desc.Hq, desc.D)
+    torch, z = _torch(), _sizes_of(desc)
+    bf16, i32 = torch.bfloat16, torch.int32
     _check(lib().bass_paged_verify_attention(
-        ctypes.byref(desc), _dev(Q, "Q", torch.bfloat16, q), *_pool_ptrs(Kpool, Vpool, desc),
-        _dev(tables, "tables", torch.int32, (desc.B, desc.max_pages)), _bytes_of(plan, bass_paged_attention_plan_bytes(desc), "plan"),
-        _dev(O, "O", torch.bfloat16, q), _dev(lse, "lse", torch.float32, q[:3], optional=True),
-        _bytes_of(workspace, 0, "workspace"), _nbytes(workspace, "workspace"), _dev(dev_status, "dev_status", torch.int32, optional=True),
+        ctypes.byref(desc), _dev(Q, "Q", bf16, z.q), _bytes_of(Kpool, z.pool, "Kpool"), _bytes_of(Vpool, z.pool, "Vpool"),
+        _dev(tables, "tables", i32, z.tables), _bytes_of(plan, z.plan, "plan"), _dev(O, "O", bf16, z.q),
+        _dev(lse, "lse", torch.float32, z.lse, optional=True), _bytes_of(workspace, 0, "workspace"), workspace.nbytes,
+        _dev(dev_status, "dev_status", i32, optional=True),
         _launch_on(stream, Q, Kpool, Vpool, tables, plan, O, lse, workspace, dev_status)), "bass_paged_verify_attention")
 
 

@@ -6,7 +6,9 @@
 
 namespace bass {
 
-constexpr int kPlanThreads2 = 1024;
+// Small batches (sequences and prefixes together) go to a workgroup of 256 threads and keep the runs in LDS too: 16 wavefronts more to start and
+// to wait for at every barrier, and a second look at the runs in memory, take 2 - 3 us of 8.
+constexpr int kSmallBatch = 256;
 
 struct PagedPlanParams {
   int B, kmax, g, Hkv, most_tokens, n_prefixes;
@@ -25,7 +27,8 @@ struct PagedPlanParams {
 struct Four {
   int v[4];
 };
-__device__ inline Four scan1024(Four x, Four* lds, Four& total) {
+template <int T>
+__device__ inline Four scan_four(Four x, Four* lds, Four& total) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   Four s = x;
 #pragma unroll
@@ -40,7 +43,7 @@ __device__ inline Four scan1024(Four x, Four* lds, Four& total) {
   __syncthreads();
   total = Four{{0, 0, 0, 0}};
 #pragma unroll
-  for (int w = 0; w < kPlanThreads2 / 64; ++w)
+  for (int w = 0; w < T / 64; ++w)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (w < wv) s.v[i] += lds[w].v[i];
@@ -51,24 +54,28 @@ __device__ inline Four scan1024(Four x, Four* lds, Four& total) {
   return s;
 }
 
-__global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanParams p) {
-  __shared__ Four sums[kPlanThreads2 / 64];
-  __shared__ int seq_L[kMaxPagedBatch], seq_n[kMaxPagedBatch], seq_g[kMaxPagedBatch];
+// T threads; at most N sequences and N prefixes.
+template <int T, int N>
+__global__ __launch_bounds__(T) void paged_plan_kernel(PagedPlanParams p) {
+  constexpr bool kRunsInLds = N <= kSmallBatch;
+  __shared__ Four sums[T / 64];
+  __shared__ PagedRun lds_runs[kRunsInLds ? N : 1];
+  __shared__ int seq_L[N], seq_n[N], seq_g[N];
   // of each prefix: least ctx_len, then common blocks; query tokens, then their first place in the list; sequences, then its run; first sequence
-  __shared__ int pre_L[kMaxPagedBatch], pre_tok[kMaxPagedBatch], pre_row[kMaxPagedBatch], pre_n[kMaxPagedBatch];
-  __shared__ int starts[2 * kMaxPagedBatch];
+  __shared__ int pre_L[N], pre_tok[N], pre_row[N], pre_n[N];
+  __shared__ int starts[2 * N];
   const int tid = threadIdx.x;
   // the first sequence of every thread, requested with the prefixes' lengths: one trip to memory
   const bool has = tid < p.B;
   const int my_L = has ? p.ctx_len[tid] : 0, my_n = has ? p.draft_len[tid] : 0, my_x = has && p.prefix_of ? p.prefix_of[tid] : -1;
-  for (int x = tid; x < p.n_prefixes; x += kPlanThreads2) {
+  for (int x = tid; x < p.n_prefixes; x += T) {
     pre_L[x] = p.prefix_len[x];
     pre_tok[x] = pre_n[x] = 0;
     pre_row[x] = 1 << 30;
   }
   __syncthreads();
   int bad = 0;
-  for (int b = tid; b < p.B; b += kPlanThreads2) {
+  for (int b = tid; b < p.B; b += T) {
     int L = b == tid ? my_L : p.ctx_len[b], n = b == tid ? my_n : p.draft_len[b];
     if (clamp_lengths(L, n, p.kmax, p.most_tokens)) bad = BASS_STATUS_LEN_CLAMPED;
     int x = b == tid ? my_x : p.prefix_of ? p.prefix_of[b] : -1;
@@ -87,7 +94,7 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
   if (bad && p.status) atomicOr(p.status, bad);
   __syncthreads();
   // common blocks of a prefix's sequences; 0: they go by themselves
-  for (int x = tid; x < p.n_prefixes; x += kPlanThreads2)
+  for (int x = tid; x < p.n_prefixes; x += T)
     pre_L[x] = pre_n[x] >= 2 && pre_L[x] >= kLeastShared * kBlockTokens ? pre_L[x] / kBlockTokens : 0;
   __syncthreads();
 
@@ -98,7 +105,7 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
   for (int pass = p.n_prefixes > 0 ? 0 : 1; pass < 2; ++pass) {
     per = min(entries / kPagedShares, 1 << 20);
     n_runs = entries = rows = listed = 0;
-    for (int x0 = 0; x0 < items; x0 += kPlanThreads2) {
+    for (int x0 = 0; x0 < items; x0 += T) {
       const int x = x0 + tid, b = x - p.n_prefixes;
       PagedRun r{};
       int units = 0, list = 0;
@@ -131,7 +138,7 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
       if (pass == 1 && r.tile_tok * p.g > kWaveRows) r.cost = tile_cost(r.cost, per);
       r.pad = unit_pad(r.tile_tok * p.g, r.heads);
       Four total;
-      const Four before = scan1024(Four{{units > 0, units * r.entries(), units > 0 ? r.n_tok * p.g * p.Hkv : 0, list}}, sums, total);
+      const Four before = scan_four<T>(Four{{units > 0, units * r.entries(), units > 0 ? r.n_tok * p.g * p.Hkv : 0, list}}, sums, total);
       const int at = n_runs + before.v[0], place = listed + before.v[3];
       r.start = entries + before.v[1];
       r.row_base = rows + before.v[2];
@@ -147,6 +154,7 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
       }
       if (units > 0) {
         p.runs[at] = r;
+        if constexpr (kRunsInLds) lds_runs[at] = r;
         starts[at] = r.start;
       }
       if (x >= p.n_prefixes && x < items) p.seqs[b] = PagedSeq{seq_n[b], 0, {0, 0}, r, PagedRun{}};
@@ -155,14 +163,15 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
   __syncthreads();
 
   // Token lists of the shared runs: a sequence's tokens stand behind those of the sequences before it.
-  for (int b = tid; b < p.B; b += kPlanThreads2) {
+  for (int b = tid; b < p.B; b += T) {
     const int x = seq_g[b];
     if (x < 0 || pre_n[x] < 0) continue;
     int pos = 0;
 #pragma unroll 8
     for (int o = pre_row[x]; o < b; ++o) pos += seq_g[o] == x ? seq_n[o] : 0;
     for (int i = 0; i < seq_n[b]; ++i) p.tokens[pre_tok[x] + pos + i] = b * p.kmax + i;
-    p.seqs[b].shared = p.runs[pre_n[x]];
+    if constexpr (kRunsInLds) p.seqs[b].shared = lds_runs[pre_n[x]];
+    else p.seqs[b].shared = p.runs[pre_n[x]];
     p.seqs[b].pos = pos;
   }
 
@@ -179,7 +188,7 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
     h.used = used;
     *p.header = h;
   }
-  for (int w = tid; w < kPagedShares; w += kPlanThreads2) {
+  for (int w = tid; w < kPagedShares; w += T) {
     PagedShare s{};
     s.signature = p.signature;
     const int x0 = w < used ? split.first(w) : entries, x1 = w < used ? split.first(w + 1) : entries;
@@ -192,7 +201,8 @@ __global__ __launch_bounds__(kPlanThreads2) void paged_plan_kernel(PagedPlanPara
         else hi = m - 1;
       }
       s.run = lo;
-      s.first = p.runs[lo];
+      if constexpr (kRunsInLds) s.first = lds_runs[lo];
+      else s.first = p.runs[lo];
       s.unit = (x0 - s.first.start) / s.first.entries();
       s.off = (x0 - s.first.start) % s.first.entries();
     }
@@ -222,6 +232,8 @@ extern "C" int bass_paged_attention_plan(const bass_paged_desc* d, const int32_t
                      d->dtype == BASS_DTYPE_INT8KV, paged_signature(d),
                     ctx_len, draft_len, prefix_of, prefix_len, (PagedHeader*)at, (PagedShare*)(at + l.shares), (PagedRun*)(at + l.runs),
                     (PagedSeq*)(at + l.seqs), (int32_t*)(at + l.tokens), dev_status};
-  hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads2), 0, (hipStream_t)stream, p);
+  // a batch of N sequences and prefixes has at most N runs
+  if (d->B + n_prefixes <= kSmallBatch) hipLaunchKernelGGL((paged_plan_kernel<256, kSmallBatch>), dim3(1), dim3(256), 0, (hipStream_t)stream, p);
+  else hipLaunchKernelGGL((paged_plan_kernel<1024, kMaxPagedBatch>), dim3(1), dim3(1024), 0, (hipStream_t)stream, p);
   return launch_status();
 }
