@@ -618,12 +618,16 @@ __global__ __launch_bounds__(64 * kPagedWaves, 1) void paged_attn(PagedParams p)
     const PagedSegment s = paged_segment(run, unit, off, entries);
     if (s.n > 0) {
       const int rows = s.n_tok * p.g;
-      if (rows <= 32 && run.heads > 1) paged_unit<D, kI8, 1, true>(p, s, blockIdx.x, lds.one);
-      else if (rows <= 32) paged_unit<D, kI8, 1, false>(p, s, blockIdx.x, lds.one);
-      else if (rows <= kWaveRows && run.heads > 1) paged_unit<D, kI8, 2, true>(p, s, blockIdx.x, lds.two);
-      else if (rows <= kWaveRows) paged_unit<D, kI8, 2, false>(p, s, blockIdx.x, lds.two);
-      else if (rows <= kTileRows / 2) paged_tile<D, kI8, 1>(p, s, blockIdx.x, lds.tile);
-      else paged_tile<D, kI8, 2>(p, s, blockIdx.x, lds.tile);
+      if (is_tile(run.L < 0, run.tile_tok * p.g)) {
+        if (run.tile_tok * p.g <= kTileRows / 2) paged_tile<D, kI8, 1>(p, s, blockIdx.x, lds.tile);
+        else paged_tile<D, kI8, 2>(p, s, blockIdx.x, lds.tile);
+      } else if (rows <= 32) {
+        if (run.heads > 1) paged_unit<D, kI8, 1, true>(p, s, blockIdx.x, lds.one);
+        else paged_unit<D, kI8, 1, false>(p, s, blockIdx.x, lds.one);
+      } else {
+        if (run.heads > 1) paged_unit<D, kI8, 2, true>(p, s, blockIdx.x, lds.two);
+        else paged_unit<D, kI8, 2, false>(p, s, blockIdx.x, lds.two);
+      }
     }
     entries -= run.entries() - off;
     if (entries <= 0) break;

@@ -19,12 +19,17 @@ constexpr int kPagedShares = 256;   // workgroups of the attention launch: one p
 constexpr int kCostRows1 = 4, kCostRows2 = 6, kCostTile1 = 6, kCostTile2 = 8, kCostTile1Int8 = 9, kCostTile2Int8 = 13;
 constexpr int kPadHeads = 32, kPadRows = 40, kPadTile = 76;
 constexpr int kTileStart = 48;  // a workgroup that begins with a tile loses so much more than one that begins with few rows (see tile_cost)
-// Runs of at most so many blocks give each wavefront a kv head: nothing is merged, but a workgroup has four partial results.
-constexpr int kHeadBlocks = 48;
+// Short runs give each wavefront a kv head of its own: nothing is merged, but a workgroup has four partial results, and the list has fewer, longer
+// units.  Worth it where units are many.  us per layer, heads of 128, 4 tokens, without -> with: 32/8 heads, 32 sequences of 40 / 100 / 200 / 400 tokens
+// 15.4 / 16.3 / 18.7 / 21.7 -> 14.2 / 16.6 / 18.6 / 23.9; 128 sequences 33.2 / 37.4 / 45.2 / 55.5 -> 23.4 / 29.2 / 37.2 / 52.7; 4 sequences 9.1 / 10.9 / 12.7 / 13.4 ->
+// 11.7 / 12.3 / 13.7 / 14.2; 64 rows, 128 sequences 54.8 / 59.6 / 68.6 / 80.8 -> 40.9 / 48.8 / 55.3 / 75.7; 24 sequences of 40 / 200 / 400 tokens, 16 rows
+// 10.9 / 16.1 / 19.3 -> 13.9 / 17.2 / 21.2.  So where there is about a unit per workgroup, up to 8 blocks, and twice as many with more than 32 rows, whose states
+// are twice as large to merge, or with four times the units.
+constexpr int kHeadUnits = 240, kHeadBlocks = 8;
+BASS_HD inline int head_blocks(int units, int rows) { return units < kHeadUnits ? 0 : rows > 32 || units >= 4 * kHeadUnits ? 2 * kHeadBlocks : kHeadBlocks; }
 constexpr int kLeastEntries = 40;   // of a workgroup, as long as there are fewer workgroups than kPagedShares; at least the largest cost
 constexpr int kTileRows = 256;      // most query rows of a tile
 constexpr int kSlotRows = kTileRows;  // rows between the partial results of two workgroups (see partial_row)
-constexpr int kLeastShared = 4;     // a common prefix of fewer blocks is left to the sequences themselves
 
 struct PagedRun {
   int32_t row;       // whose table is read
@@ -46,12 +51,27 @@ struct PagedRun {
   BASS_HD int block_at(int entry) const { return imin((entry + cost - 1) / cost, n_blk); }  // first block that starts at `entry` or behind it
 };
 
-constexpr int kWaveRows = 64;  // up to so many rows of a tile every wavefront has all of them
-BASS_HD inline int block_cost(int tile_rows, int heads, bool int8) {
-  if (tile_rows <= kWaveRows) return (tile_rows <= kWaveRows / 2 ? kCostRows1 : kCostRows2) * heads;
-  return tile_rows <= kTileRows / 2 ? (int8 ? kCostTile1Int8 : kCostTile1) : int8 ? kCostTile2Int8 : kCostTile2;
+constexpr int kTileFrom = 32;  // shared runs: tiles where a tile has more rows
+BASS_HD inline bool is_tile(bool shared, int rows) { return shared && rows > kTileFrom; }
+BASS_HD inline int block_cost(bool shared, int rows, int heads, bool int8) {
+  if (!is_tile(shared, rows)) return (rows <= 32 ? kCostRows1 : kCostRows2) * heads;
+  return rows <= kTileRows / 2 ? (int8 ? kCostTile1Int8 : kCostTile1) : int8 ? kCostTile2Int8 : kCostTile2;
 }
-BASS_HD inline int unit_pad(int tile_rows, int heads) { return tile_rows > kWaveRows ? kPadTile : heads > 1 ? kPadHeads : kPadRows; }
+BASS_HD inline int unit_pad(bool shared, int rows, int heads) { return is_tile(shared, rows) ? kPadTile : heads > 1 ? kPadHeads : kPadRows; }
+// Whether a common prefix is computed for all of its sequences together.  Separate sequences read it again from the caches; together, a workgroup has one
+// more beginning and end, and every row one more partial result.  us per layer, separate / together, prefixes of 256 / 512 / 1024 / 2048 / 4096 tokens, 200
+// of their own, 4 query tokens: 32 heads, 2 sequences 13.1 / 13.8 / 14.3 / 16.9 / 22.8 and 13.8 / 14.1 / 14.4 / 17.1 / 22.1, 4 sequences 14.5 / 15.3 / 17.7 / 22.3 / 31.9 and 14.6 /
+// 14.5 / 15.5 / 19.3 / 24.2, 8 sequences 19.2 / 23.0 / 30.9 / 48.2 / 81.9 and 16.8 / 16.7 / 18.8 / 20.9 / 26.3; 32/8 heads, 8 sequences 13.6 / 14.8 / 16.0 / 20.2 / 28.0 and 14.9 / 16.6 / 19.7 /
+// 22.7 / 27.1, 32 sequences 22.2 / 26.0 / 33.6 / 51.9 / 89.2 and 26.1 / 27.9 / 29.2 / 34.2 / 37.4; 64/8 heads, 8 sequences 14.0 / 15.5 / 17.4 / 22.0 / 29.4 and 21.3 / 23.5 / 26.7 / 28.0 /
+// 32.9, 32 sequences 24.9 / 29.1 / 37.5 / 55.5 / 94.3 and 28.7 / 33.8 / 36.2 / 39.6 / 49.4.  In entries saved per workgroup: from about 20 on, or 100 with tiles, whose
+// beginnings are long; but those are paid once for all prefixes of a batch.
+constexpr int kSavedRows = 20, kSavedTile = 100;
+BASS_HD inline int saved_by_sharing(int members, int tokens, int tiles, int tile_tok, int n_blk, int g, int Hkv, bool int8) {
+  const int64_t apart = (int64_t)members * block_cost(false, tokens * g / members, 1, int8), together = (int64_t)tiles * block_cost(true, tile_tok * g, 1, int8);
+  const int64_t saved = (apart - together) * n_blk * Hkv / kPagedShares;
+  return saved < 0 ? 0 : (int)(saved < (1 << 16) ? saved : 1 << 16);
+}
+BASS_HD inline bool worth_sharing(int saved, int saved_by_all, bool tile) { return saved >= kSavedRows && saved_by_all >= (tile ? kSavedTile : kSavedRows); }
 // Every workgroup pays for a beginning, those with tiles more; in short lists that is much of their time, so that a tile's block counts for more there.
 // per: entries of a workgroup by the plain costs.
 BASS_HD inline int tile_cost(int cost, int per) { return (int)((int64_t)cost * per / imax(per - kTileStart, per / 3 + 1)) + 1; }

@@ -63,11 +63,12 @@ __global__ __launch_bounds__(T) void paged_plan_kernel(PagedPlanParams p) {
   __shared__ int seq_L[N], seq_n[N], seq_g[N];
   // of each prefix: least ctx_len, then common blocks; query tokens, then their first place in the list; sequences, then its run; first sequence
   __shared__ int pre_L[N], pre_tok[N], pre_row[N], pre_n[N];
-  __shared__ int starts[2 * N];
+  __shared__ int starts[2 * N], live, saved_all;  // live: sequences with query tokens, and tiles of shared runs
   const int tid = threadIdx.x;
   // the first sequence of every thread, requested with the prefixes' lengths: one trip to memory
   const bool has = tid < p.B;
   const int my_L = has ? p.ctx_len[tid] : 0, my_n = has ? p.draft_len[tid] : 0, my_x = has && p.prefix_of ? p.prefix_of[tid] : -1;
+  if (tid == 0) live = saved_all = 0;
   for (int x = tid; x < p.n_prefixes; x += T) {
     pre_L[x] = p.prefix_len[x];
     pre_tok[x] = pre_n[x] = 0;
@@ -84,6 +85,7 @@ __global__ __launch_bounds__(T) void paged_plan_kernel(PagedPlanParams p) {
     seq_L[b] = L;
     seq_n[b] = n;
     seq_g[b] = x;
+    if (n > 0) atomicAdd(&live, 1);
     if (x >= 0) {
       atomicMin(&pre_L[x], L);
       atomicAdd(&pre_tok[x], n);
@@ -93,12 +95,33 @@ __global__ __launch_bounds__(T) void paged_plan_kernel(PagedPlanParams p) {
   }
   if (bad && p.status) atomicOr(p.status, bad);
   __syncthreads();
-  // common blocks of a prefix's sequences; 0: they go by themselves
-  for (int x = tid; x < p.n_prefixes; x += T)
-    pre_L[x] = pre_n[x] >= 2 && pre_L[x] >= kLeastShared * kBlockTokens ? pre_L[x] / kBlockTokens : 0;
+  // Common blocks of a prefix's sequences; 0: they go by themselves.  And the tiles of their query tokens.
+  auto tiles_of = [&](int tokens, int& tile_tok) {
+    const int n = (tokens * p.g + kTileRows - 1) / kTileRows;
+    tile_tok = min((tokens + n - 1) / n, kTileRows / p.g);
+    return (tokens + tile_tok - 1) / tile_tok;
+  };
+  auto saved_by = [&](int x, int& blocks, bool& tile) {
+    blocks = pre_n[x] >= 2 ? max(pre_L[x], 0) / kBlockTokens : 0;
+    if (blocks == 0) return 0;
+    int tile_tok;
+    const int tiles = tiles_of(pre_tok[x], tile_tok);
+    tile = is_tile(true, tile_tok * p.g);
+    return saved_by_sharing(pre_n[x], pre_tok[x], tiles, tile_tok, blocks, p.g, p.Hkv, p.int8);
+  };
+  int blocks;
+  bool tile = false;
+  for (int x = tid; x < p.n_prefixes; x += T) atomicAdd(&saved_all, saved_by(x, blocks, tile));
   __syncthreads();
+  for (int x = tid; x < p.n_prefixes; x += T) {
+    const int saved = saved_by(x, blocks, tile);
+    pre_L[x] = worth_sharing(saved, saved_all, tile) ? blocks : 0;
+    int tile_tok;
+    if (pre_L[x] > 0) atomicAdd(&live, tiles_of(pre_tok[x], tile_tok));
+  }
+  __syncthreads();
+  const int units_all = live * p.Hkv;  // with a unit for every kv head
 
-  // Runs: item x < n_prefixes is a prefix, the others are the sequences.
   // Two passes where there are prefixes: the first finds how long the list is by the plain costs.
   int n_runs = 0, entries = 0, rows = 0, listed = 0, per = 0;
   const int items = p.n_prefixes + p.B;
@@ -114,9 +137,7 @@ __global__ __launch_bounds__(T) void paged_plan_kernel(PagedPlanParams p) {
         if (r.n_blk > 0) {
           r.row = pre_row[x];
           r.n_tok = list = pre_tok[x];
-          r.n_tiles = (r.n_tok * p.g + kTileRows - 1) / kTileRows;
-          r.tile_tok = min((r.n_tok + r.n_tiles - 1) / r.n_tiles, kTileRows / p.g);
-          r.n_tiles = (r.n_tok + r.tile_tok - 1) / r.tile_tok;
+          r.n_tiles = tiles_of(r.n_tok, r.tile_tok);
           r.L = -1;
         }
       } else if (x < items && seq_n[b] > 0) {
@@ -130,13 +151,16 @@ __global__ __launch_bounds__(T) void paged_plan_kernel(PagedPlanParams p) {
         r.n_blk = num_blocks(seq_L[b] + seq_n[b]) - shared;
         r.whole = shared == 0;
       }
+      const bool shared_run = r.L < 0;
+      const int tile_rows = r.tile_tok * p.g;
+      const bool tile = is_tile(shared_run, tile_rows);
       if (r.n_tok > 0) {
-        r.heads = p.Hkv > 1 && r.n_blk <= kHeadBlocks && r.tile_tok * p.g <= kWaveRows ? kPagedWaves : 1;
+        r.heads = p.Hkv > 1 && !tile && r.n_blk <= head_blocks(units_all, tile_rows) ? kPagedWaves : 1;
         units = r.n_tiles * ((p.Hkv + r.heads - 1) / r.heads);
       }
-      r.cost = block_cost(r.tile_tok * p.g, r.heads, p.int8);
-      if (pass == 1 && r.tile_tok * p.g > kWaveRows) r.cost = tile_cost(r.cost, per);
-      r.pad = unit_pad(r.tile_tok * p.g, r.heads);
+      r.cost = block_cost(shared_run, tile_rows, r.heads, p.int8);
+      if (pass == 1 && tile) r.cost = tile_cost(r.cost, per);
+      r.pad = unit_pad(shared_run, tile_rows, r.heads);
       Four total;
       const Four before = scan_four<T>(Four{{units > 0, units * r.entries(), units > 0 ? r.n_tok * p.g * p.Hkv : 0, list}}, sums, total);
       const int at = n_runs + before.v[0], place = listed + before.v[3];
