@@ -70,6 +70,10 @@ class Batch:
         O, lse = pg.verify(hip.to_device(self.Q), hip.i32(self.tables), hip.i32(self.ctx), hip.i32(self.nq), of, plen, want_lse)
         return wl.bf16_bits_to_f32(hip.to_host(O)), hip.to_host(lse), int(pg.status.item())
 
+    def shared_runs(self, pg):
+        """Prefixes that the plan computes for all of their sequences: its second word counts the runs, one per live sequence more or less."""
+        return int(pg.plan[:8].cpu().numpy().view(np.int32)[1]) - int((self.nq > 0).sum())
+
     def reference(self):
         """(O, lse, A) in 64 bits."""
         x = [wl.bf16_bits_to_f32(y) for y in (self.Q, self.K, self.V)]
@@ -222,3 +226,244 @@ def test_lengths_are_clamped_and_prefix_numbers_checked(hip):
     ref, _, A = batch.reference()
     assert (np.abs(O - ref) <= 2 ** -6 * A + 1e-30).all()
     torch.cuda.synchronize()
+
+
+# Query rows per kv head and prefix sizes that take each of the ways: rows of at most 32 (a wavefront has all of them), half a tile of 128 rows and a
+# full one, part of a tile of 256 rows, two and three tiles; odd and even numbers of blocks, more than a window of 64.
+# members, query tokens, heads, kv heads, prefix tokens
+KINDS = [(4, 7, 16, 16, 992), (4, 10, 32, 32, 3712), (4, 16, 32, 32, 3680), (8, 8, 32, 16, 2272), (13, 4, 32, 8, 2688), (19, 4, 32, 8, 2080), (40, 4, 32, 8, 1088)]
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("int8kv", 128), ("int8kv", 64)])
+@pytest.mark.parametrize("n,q,Hq,Hkv,P", KINDS)
+def test_every_way_of_sharing(hip, dtype, D, n, q, Hq, Hkv, P):
+    rng = np.random.default_rng([n, q, P])
+    ctx = P + rng.integers(0, 40, size=n)
+    nq = rng.integers(max(1, q - 1), q + 1, size=n)
+    nq[0] = q
+    batch = Batch(n + P, Hq, Hkv, D, 32, ctx, nq, q, np.zeros(n, int), [P], dtype)
+    pg = batch.pages(hip)
+    batch.check(hip, pg=pg)
+    assert batch.shared_runs(pg) == 1
+
+
+def test_the_same_call_gives_the_same_bits(hip):
+    """Nothing depends on the order in which workgroups arrive.  (Equal sequences agree up to rounding only: the list is cut at other blocks of each.)"""
+    n = 24
+    batch = Batch(3, 32, 8, 128, 64, [2048 + 37] * n, [4] * n, 4, np.zeros(n, int), [2048])
+    pg = batch.pages(hip)
+    O, lse = batch.check(hip, pg=pg)
+    assert batch.shared_runs(pg) == 1
+    for _ in range(3):
+        pg.ws.fill_(0xFF)
+        O2, lse2, _ = batch.run(hip, pg)
+        assert np.array_equal(O, O2) and np.array_equal(lse, lse2)
+
+
+def test_large_batches_and_many_prefixes(hip):
+    """More sequences and prefixes than the small planning kernel takes; half of them not in use."""
+    rng = np.random.default_rng(4)
+    n, G = 300, 40
+    of = rng.integers(-1, G, size=n)
+    plen = rng.integers(1, 5, size=G) * 32
+    ctx = np.where(of >= 0, plen[of], 0) + rng.integers(0, 60, size=n)
+    Batch(21, 8, 4, 64, 32, ctx, rng.integers(0, 3, size=n), 2, of, plen).check(hip)
+
+
+@pytest.mark.parametrize("n,P", [(2, 64), (16, 2048)])
+def test_scores_of_any_finite_size(hip, n, P):
+    """Products that are exact in 32 bits, up to 2^31: one key wins, the output is its value row.  Apart and together."""
+    rng = np.random.default_rng(n)
+    batch = Batch(n, 32, 8, 64, 32, [P + 20] * n, [4] * n, 4, np.zeros(n, int), [P], scale=1.0)
+    f = np.zeros(batch.Q.shape, np.float32)
+    f[..., 0] = 2.0 ** 24
+    batch.Q = wl.to_bf16_bits(f)
+    k = np.zeros(batch.K.shape, np.float32)
+    k[..., 0] = rng.integers(-60, 60, size=k.shape[:-1])
+    winner = rng.integers(0, P + 20, size=n)
+    k[:, :P] = k[0, :P]
+    for b in range(n):
+        k[b, winner[b] if winner[b] >= P else winner[0] % P, :, 0] = 100 + (b if winner[b] >= P else 0) % 20
+    k[:, :P] = k[0, :P]
+    k[:, winner[0] % P, :, 0] = 90
+    batch.K = wl.to_bf16_bits(k)
+    pg = batch.pages(hip)
+    O, lse, status = batch.run(hip, pg)
+    assert status == 0 and batch.shared_runs(pg) == (1 if n > 2 else 0)
+    v = wl.bf16_bits_to_f32(batch.V)
+    for b in range(n):
+        for h in range(8):
+            for i in range(4):
+                row = k[b, :P + 21 + i, h, 0]
+                best = np.flatnonzero(row == row.max())
+                want = v[b, best, h].astype(np.float64).mean(0)
+                assert np.abs(O[b, i, 4 * h:4 * h + 4] - want).max() <= 2 ** -7 * np.abs(v[b, best, h]).max()
+
+
+@pytest.mark.parametrize("n,P", [(3, 96), (16, 2048)])
+def test_an_infinite_value_stays_infinite(hip, n, P):
+    batch = Batch(n + 50, 32, 8, 128, 32, [P + 20] * n, [4] * n, 4, np.zeros(n, int), [P])
+    v = wl.bf16_bits_to_f32(batch.V)
+    v[:, 5, 3, 77] = np.inf
+    v[1, P + 2, 1, 11] = -np.inf
+    batch.V = wl.to_bf16_bits(v)
+    pg = batch.pages(hip)
+    O, lse, _ = batch.run(hip, pg)
+    assert batch.shared_runs(pg) == (1 if n > 3 else 0)
+    want = np.zeros(O.shape, np.float32)
+    want[:, :, 12:16, 77] = np.inf
+    want[1, :, 4:8, 11] = -np.inf
+    assert np.array_equal(np.where(np.isinf(O), O, 0), want) and not np.isnan(O).any()
+
+
+def test_a_context_of_two_million_tokens(hip):
+    """More blocks per workgroup than a window of page numbers: keys are zero, so every token counts alike; a block's values are one number."""
+    import torch
+    n = 2_200_000 + 5
+    P = 4096
+    pages = n // P + 2
+    pg = hip.DevicePages(1, 2, 2, 1, 64, P, pages, pages, "bf16", 1.0)
+    blocks = pages * P // 32
+    value = torch.randint(-8, 9, (blocks,), device="cuda").float()
+    pg.V.view(torch.bfloat16).view(blocks, 32 * 64).copy_(value[:, None].expand(-1, 32 * 64))
+    tables = torch.randperm(pages, device="cuda").to(torch.int32)[None].contiguous()
+    order = (tables[0].long()[:, None] * (P // 32) + torch.arange(P // 32, device="cuda")).view(-1)
+    per_token = value[order].double().repeat_interleave(32)
+    Q = torch.randn((1, 2, 2, 64), device="cuda").to(torch.bfloat16)
+    O, lse = pg.verify(Q, tables, hip.i32([n - 2]), hip.i32([2]))
+    for i in range(2):
+        mean = per_token[:n - 1 + i].mean().item()
+        assert abs(lse[0, i].cpu().numpy() - np.log(n - 1 + i)).max() <= 2e-6
+        assert (O[0, i].float() - mean).abs().max().item() <= 2 ** -8 * abs(mean) + 1e-6 * 8
+    assert int(pg.status.item()) == 0
+
+
+def test_replayed_graph(hip):
+    """Plan and two layers captured; every replay, with other lengths and eager work between, equals the eager call bit for bit."""
+    import torch
+    import paper_2404_15778_amd as bass
+    rng = np.random.default_rng(9)
+    n = 16
+    batch = Batch(31, 32, 8, 128, 64, [2048 + 300] * n, [4] * n, 4, np.zeros(n, int), [2048])
+    pg = batch.pages(hip)
+    ctx, nq, of, plen, tables = (hip.i32(x) for x in (batch.ctx, batch.nq, batch.of, batch.plen, batch.tables))
+    Q = hip.to_device(batch.Q)
+
+    def step(plan, ws, O, lse):
+        bass.bass_paged_attention_plan(pg.desc, ctx, nq, of, plen, plan, pg.status)
+        for l in range(2):
+            bass.bass_paged_verify_attention(pg.desc, Q, pg.K, pg.V, tables, plan, O[l], lse[l], ws, pg.status)
+
+    new = lambda: ([torch.empty_like(pg.O) for _ in range(2)], [torch.empty_like(pg.lse) for _ in range(2)])  # noqa: E731
+    (O1, l1), (O2, l2) = new(), new()
+    ws2, plan2 = bass.alloc_paged_workspace(pg.desc), bass.alloc_paged_plan(pg.desc)
+    step(pg.plan, pg.ws, O1, l1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(pg.plan, pg.ws, O1, l1)
+    for _ in range(4):
+        ctx.copy_(torch.tensor(2048 + rng.integers(0, 290, size=n), dtype=torch.int32))
+        nq.copy_(torch.tensor(rng.integers(0, 5, size=n), dtype=torch.int32))
+        for x in O1 + l1:
+            x.fill_(float("nan"))
+        graph.replay()
+        step(plan2, ws2, O2, l2)
+        torch.cuda.synchronize()
+        for a, b in zip(O1 + l1, O2 + l2):
+            assert torch.equal(a, b)
+    assert int(pg.status.item()) == 0
+
+
+def test_two_streams_at_once(hip):
+    """Two batches on streams of their own, with workspaces of their own and one plan."""
+    import torch
+    import paper_2404_15778_amd as bass
+    n = 16
+    batch = Batch(41, 32, 8, 128, 64, [2048 + 100] * n, [4] * n, 4, np.zeros(n, int), [2048])
+    pg = batch.pages(hip)
+    Q = [hip.to_device(batch.Q), hip.to_device(batch.Q[::-1])]
+    tables = [hip.i32(batch.tables), hip.i32(batch.tables[::-1].copy())]
+    want = [pg.verify(Q[k], tables[k], hip.i32(batch.ctx), hip.i32(batch.nq), hip.i32(batch.of), hip.i32(batch.plen))[0].clone() for k in range(2)]
+    O = pg.O
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.empty_like(O) for _ in range(5)] for _ in range(2)]
+    ws = [bass.alloc_paged_workspace(pg.desc) for _ in range(2)]
+    torch.cuda.synchronize()
+    for r in range(5):
+        for k in range(2):
+            bass.bass_paged_verify_attention(pg.desc, Q[k], pg.K, pg.V, tables[k], pg.plan, outs[k][r], None, ws[k], pg.status, streams[k])
+    torch.cuda.synchronize()
+    for k in range(2):
+        for r in range(5):
+            assert torch.equal(outs[k][r], want[k])
+
+
+def test_tensors_of_the_wrong_kind_are_refused(hip):
+    import torch
+    import paper_2404_15778_amd as bass
+    batch = Batch(51, 4, 2, 64, 32, [40, 50], [1, 2], 2)
+    pg = batch.pages(hip)
+    Q, t = hip.to_device(batch.Q), hip.i32(batch.tables)
+    good = dict(Q=Q, Kpool=pg.K, Vpool=pg.V, tables=t, plan=pg.plan, O=pg.O, lse=pg.lse, workspace=pg.ws)
+    bad = dict(Q=Q.float(), Kpool=pg.K[:-16], Vpool=pg.V.cpu(), tables=t.long(), plan=pg.plan[:64], O=pg.O.float(), lse=pg.lse[:1], workspace=None)
+    for name, x in bad.items():
+        with pytest.raises(ValueError):
+            bass.bass_paged_verify_attention(pg.desc, **{**good, name: x})
+    with pytest.raises(ValueError):
+        bass.bass_paged_verify_attention(pg.desc, **{**good, "Q": Q.transpose(0, 1).contiguous().transpose(0, 1)})
+    with pytest.raises(bass.BassError):
+        bass.bass_paged_verify_attention(pg.desc, **{**good, "workspace": pg.ws[:64]})
+    assert torch.isnan(pg.O.float()).all()
+
+
+def test_steps_of_a_server(hip):
+    """The operators together: requests that begin with a held prompt, tables, slots, rows appended, attention; drafts that are taken back, requests
+    that end and places that are taken again, over a pool that is just large enough."""
+    import torch
+    import paper_2404_15778_amd as bass
+    rng = np.random.default_rng(12)
+    B, kmax, Hq, Hkv, D, P, most, n_pages = 6, 5, 8, 4, 64, 32, 12, 44
+    prompt = 5 * P + 7
+    pg = hip.DevicePages(B, kmax, Hq, Hkv, D, P, n_pages, most, "bf16", 0.125, poison=True)
+    dt = hip.DeviceTables(B + 1, most, P, n_pages)   # the last row holds the prompt
+    tables = dt.tables[:B]
+    draw = lambda *s: wl.to_bf16_bits(rng.standard_normal(s, dtype=np.float32))  # noqa: E731
+    pk, pv = draw(1, prompt, Hkv, D), draw(1, prompt, Hkv, D)
+    none = [0] * B
+    slots = dt.update(none + [prompt], ctx_len=none + [0], n_new=none + [prompt], kmax=prompt)
+    pg.append(hip.to_device(pk), hip.to_device(pv), slots[B:].contiguous())
+    whole = prompt // P * P                          # what can be shared
+    K, V = np.zeros((B, most * P, Hkv, D), np.uint16), np.zeros((B, most * P, Hkv, D), np.uint16)
+    ctx = np.zeros(B, int)                           # 0: the place is empty
+    for step in range(12):
+        begin = [b for b in range(B) if ctx[b] == 0 and (step == 0 or rng.random() < 0.6)]
+        new = np.zeros(B, int)
+        for b in range(B):
+            if b in begin:
+                K[b, :whole], V[b, :whole] = pk[0, :whole], pv[0, :whole]
+                ctx[b] = whole
+            if ctx[b]:
+                new[b] = rng.integers(1, kmax + 1)
+        share = [B if b in begin else -1 for b in range(B)] + [-1]
+        slots = dt.update((ctx + new).tolist() + [prompt], share, [prompt] * (B + 1), ctx.tolist() + [0], new.tolist() + [0], kmax)
+        rows = [draw(B, kmax, Hkv, D) for _ in range(2)]
+        pg.append(hip.to_device(rows[0]), hip.to_device(rows[1]), slots[:B].contiguous())
+        for b in range(B):
+            K[b, ctx[b]:ctx[b] + new[b]], V[b, ctx[b]:ctx[b] + new[b]] = rows[0][b, :new[b]], rows[1][b, :new[b]]
+        Q = draw(B, kmax, Hq, D)
+        O, lse = pg.verify(hip.to_device(Q), tables, hip.i32(ctx), hip.i32(new), hip.i32(np.where(ctx > 0, 0, -1)), hip.i32([whole]))
+        f = [wl.bf16_bits_to_f32(x) for x in (Q, K, V)]
+        Or, lser = oracle.verify_attention(*f, ctx, new, 0.125)
+        A, _ = oracle.verify_attention(f[0], f[1], np.abs(f[2]), ctx, new, 0.125)
+        got = wl.bf16_bits_to_f32(hip.to_host(O))
+        assert (np.abs(got - Or) <= (2 ** -8 * (1 + 2 ** -8) + 2 ** -10) * A + 2 ** -8 * np.abs(Or) + 1e-30).all(), step
+        for b in range(B):
+            if ctx[b]:
+                ctx[b] += rng.integers(0, new[b] + 1)  # the others are taken back: written over by the next step
+                if rng.random() < 0.2 or ctx[b] + kmax > most * P:
+                    ctx[b] = 0
+    assert int(pg.status.item()) == 0 and int(dt.status.item()) == 0
+    dt.update([0] * (B + 1))
+    assert not dt.refs.any() and not dt.held.any() and (dt.tables == -1).all()
+    assert bass.STATUS_NO_PAGES == 32 and torch.cuda.is_available()
