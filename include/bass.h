@@ -379,7 +379,8 @@ int bass_paged_gather_int8(const bass_paged_desc* desc, const void* Kpool, const
 
 /*
  * Verification attention over paged caches; what bass_verify_attention computes, with O [B, kmax, Hq, D] in bf16, as the output
- * projection takes it.  The step's own K/V rows have been appended (bass_paged_append).
+ * projection takes it.  The step's own K/V rows have been appended (bass_paged_append).  INT8 pools: queries are quantized per row as in
+ * BASS_DTYPE_INT8KV, but with inv = 127 * (1 / amax), two rounded steps, for 127 / amax: codes differ where x * 127 / amax is within a rounding of a half.
  *
  * bass_paged_attention_plan: the division of a step's work over the GPU, one small launch for all layers.
  *   ctx_len, draft_len [B]    as in bass_verify_attention; ctx_len + draft_len <= max_pages * page_tokens (else clamped, BASS_STATUS_LEN_CLAMPED)

@@ -75,7 +75,8 @@ __device__ inline int token_of(const PagedParams& p, const PagedSegment& s, int 
 }
 
 // Operand B of the score tiles.  A lane's row is c of each tile, and its two lanes (h) have the row's 16-byte chunks in turn.  A negative softmax
-// scale is moved into the queries (exact), and so is a zero; the factor that is left is positive.  INT8: quantized like cached rows.
+// scale is moved into the queries (exact), and so is a zero; the factor that is left is positive.  INT8: quantized per row, with 127 (1 / amax) for the
+// cached rows' 127 / amax: the codes are the same but where x 127 / amax is a half to within its roundings.
 template <int D, bool kI8, int NT>
 __device__ inline void load_paged_queries(const PagedParams& p, const PagedSegment& s, int kvh, int c, int h, WideQueries<D, kI8, NT>& q) {
   using G = Wide<D, kI8, NT>;
@@ -98,7 +99,7 @@ __device__ inline void load_paged_queries(const PagedParams& p, const PagedSegme
       }
       amax = G::row_max(amax);
       const float scale = amax / 127.0f * fabsf(p.scale_log2);
-      const float inv = amax > 0.f && scale != 0.f ? 127.0f / amax : 0.f;
+      const float inv = amax > 0.f && scale != 0.f ? 1.0f / amax * 127.0f : 0.f;  // a division and a product, each rounded
       q.row_scale[nt] = scale != 0.f ? scale : 1.f;
 #pragma unroll
       for (int x = 0; x < G::kQuerySteps; ++x) {

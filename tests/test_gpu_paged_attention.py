@@ -21,6 +21,14 @@ def hip():
     return harness
 
 
+def quantize_queries(x):
+    """Codes and scales of query rows over INT8 pools: as of cached rows, with 127 * (1 / amax) in two rounded steps."""
+    amax = np.abs(x).max(axis=-1).astype(np.float32)
+    with np.errstate(divide="ignore"):
+        inv = np.where(amax > 0, (np.float32(1) / amax).astype(np.float32) * np.float32(127), np.float32(0)).astype(np.float32)
+    return np.rint(x * inv[..., None]).astype(np.int8), (amax / np.float32(127)).astype(np.float32)
+
+
 class Batch:
     """Sequences with common prefixes: logical rows, tables over pages in random order, and the references."""
 
@@ -78,7 +86,7 @@ class Batch:
         """(O, lse, A) in 64 bits."""
         x = [wl.bf16_bits_to_f32(y) for y in (self.Q, self.K, self.V)]
         if self.dtype == "int8kv":
-            x = [dequantize_rows(*quantize_rows(y)) for y in x]
+            x = [dequantize_rows(*f(y)) for f, y in zip((quantize_queries, quantize_rows, quantize_rows), x)]
         O, lse = oracle.verify_attention(*x, self.ctx, self.nq, self.scale)
         A, _ = oracle.verify_attention(x[0], x[1], np.abs(x[2]), self.ctx, self.nq, self.scale)
         return O, lse, A
