@@ -542,28 +542,56 @@ def _sizes_of(desc):
     return _paged_sizes(bytes(desc))
 
 
-def _bytes_of(t, need, name):
-    """Device pointer of a contiguous GPU tensor of any type that holds at least `need` bytes."""
-    if t is None or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous GPU tensor")
+def _current():
+    """The current GPU: all tensors of a call have to live there, since a launch goes to one of its streams."""
+    try:
+        return _torch()._C._cuda_getDevice()
+    except RuntimeError:  # there is none: every tensor is refused
+        return None
+
+
+def _elsewhere(t, name):
+    raise ValueError(f"{name} must live on the current GPU" if t.is_cuda else f"{name} must live on the GPU")
+
+
+def _at(t, name, dev, dtype, shape=None):
+    """Device pointer of a contiguous tensor on GPU `dev` after dtype / shape checks (shape: a tuple)."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.get_device() != dev:
+        _elsewhere(t, name)
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _at_or_none(t, name, dev, dtype, shape=None):
+    return None if t is None else _at(t, name, dev, dtype, shape)
+
+
+def _bytes_of(t, need, name, dev):
+    """Device pointer of a contiguous tensor of any type on GPU `dev` that holds at least `need` bytes."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.get_device() != dev:
+        _elsewhere(t, name)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
     if t.nbytes < need:
         raise ValueError(f"{name} holds {t.nbytes} bytes, {need} are needed")
     return t.data_ptr()
 
 
-def _launch_on(stream, anchor, *others):
-    """The stream of a call on `anchor`'s device.  All tensors have to be there, and it has to be the current device, whose stream a
-    launch goes to."""
-    index = anchor.get_device()
-    for t in others:
-        if t is not None and t.get_device() != index:
-            raise ValueError("all tensors of a call must live on the same GPU")
-    c = _torch()._C
-    if index != c._cuda_getDevice():
-        raise ValueError("the tensors must live on the current GPU (torch.cuda.device)")
-    if stream is None:
-        return c._cuda_getCurrentRawStream(index)
-    return getattr(stream, "cuda_stream", stream)
+def _status_at(t, dev):
+    if t is None:
+        return None
+    if t.numel() < 1:
+        raise ValueError("dev_status must hold a word")
+    return _at(t, "dev_status", dev, _torch_module.int32)
 
 
 def bass_page_tables(length, held, tables, refs, page_tokens, workspace, share_from=None, share_len=None, ctx_len=None, n_new=None, slots=None,
@@ -575,73 +603,67 @@ def bass_page_tables(length, held, tables, refs, page_tokens, workspace, share_f
         raise ValueError("tables must be [rows, max_pages] and refs [n_pages]")
     if slots is not None and (slots.dim() != 2 or ctx_len is None or n_new is None):
         raise ValueError("slots must be [rows, kmax] and needs ctx_len and n_new")
-    rows, max_pages = tables.shape
-    n_pages, kmax = refs.shape[0], 0 if slots is None else slots.shape[1]
+    dev = _current()
+    (rows, max_pages), n_pages, kmax = tables.shape, refs.shape[0], 0 if slots is None else slots.shape[1]
     one = (rows,)
-    args = (_dev(length, "length", i32, one), _dev(share_from, "share_from", i32, one, optional=True),
-            _dev(share_len, "share_len", i32, one, optional=True), _dev(held, "held", i32, one), _dev(tables, "tables", i32),
-            _dev(refs, "refs", i32), kmax, _dev(ctx_len, "ctx_len", i32, one, optional=True), _dev(n_new, "n_new", i32, one, optional=True),
-            _dev(slots, "slots", i32, (rows, kmax), optional=True))
-    ws = _bytes_of(workspace, 0, "workspace")
     _check(lib().bass_page_tables(
-        rows, max_pages, int(page_tokens), n_pages, *args, ws, workspace.nbytes, _dev(dev_status, "dev_status", i32, optional=True),
-        _launch_on(stream, tables, length, share_from, share_len, held, refs, ctx_len, n_new, slots, workspace, dev_status)), "bass_page_tables")
+        rows, max_pages, int(page_tokens), n_pages, _at(length, "length", dev, i32, one), _at_or_none(share_from, "share_from", dev, i32, one),
+        _at_or_none(share_len, "share_len", dev, i32, one), _at(held, "held", dev, i32, one), _at(tables, "tables", dev, i32),
+        _at(refs, "refs", dev, i32), kmax, _at_or_none(ctx_len, "ctx_len", dev, i32, one), _at_or_none(n_new, "n_new", dev, i32, one),
+        _at_or_none(slots, "slots", dev, i32, (rows, kmax)), _bytes_of(workspace, 0, "workspace", dev), workspace.nbytes,
+        _status_at(dev_status, dev), _stream(stream)), "bass_page_tables")
 
 
 def bass_paged_append(desc, Kpool, Vpool, K_new, V_new, slots, dev_status=None, stream=None):
-    torch, z = _torch(), _sizes_of(desc)
-    bf16, i32 = torch.bfloat16, torch.int32
+    torch, z, dev = _torch(), _sizes_of(desc), _current()
+    bf16 = torch.bfloat16
     _check(lib().bass_paged_append(
-        ctypes.byref(desc), _bytes_of(Kpool, z.pool, "Kpool"), _bytes_of(Vpool, z.pool, "Vpool"), _dev(K_new, "K_new", bf16, z.rows),
-        _dev(V_new, "V_new", bf16, z.rows), _dev(slots, "slots", i32, z.slots), _dev(dev_status, "dev_status", i32, optional=True),
-        _launch_on(stream, Kpool, Vpool, K_new, V_new, slots, dev_status)), "bass_paged_append")
+        ctypes.byref(desc), _bytes_of(Kpool, z.pool, "Kpool", dev), _bytes_of(Vpool, z.pool, "Vpool", dev), _at(K_new, "K_new", dev, bf16, z.rows),
+        _at(V_new, "V_new", dev, bf16, z.rows), _at(slots, "slots", dev, torch.int32, z.slots), _status_at(dev_status, dev), _stream(stream)),
+        "bass_paged_append")
 
 
 def bass_paged_gather(desc, Kpool, Vpool, K_out, V_out, tables, start, n, dev_status=None, stream=None):
-    torch, z = _torch(), _sizes_of(desc)
+    torch, z, dev = _torch(), _sizes_of(desc), _current()
     bf16, i32 = torch.bfloat16, torch.int32
     _check(lib().bass_paged_gather(
-        ctypes.byref(desc), _bytes_of(Kpool, z.pool, "Kpool"), _bytes_of(Vpool, z.pool, "Vpool"), _dev(K_out, "K_out", bf16, z.rows),
-        _dev(V_out, "V_out", bf16, z.rows), _dev(tables, "tables", i32, z.tables), _dev(start, "start", i32, z.batch), _dev(n, "n", i32, z.batch),
-        _dev(dev_status, "dev_status", i32, optional=True),
-        _launch_on(stream, Kpool, Vpool, K_out, V_out, tables, start, n, dev_status)), "bass_paged_gather")
+        ctypes.byref(desc), _bytes_of(Kpool, z.pool, "Kpool", dev), _bytes_of(Vpool, z.pool, "Vpool", dev), _at(K_out, "K_out", dev, bf16, z.rows),
+        _at(V_out, "V_out", dev, bf16, z.rows), _at(tables, "tables", dev, i32, z.tables), _at(start, "start", dev, i32, z.batch),
+        _at(n, "n", dev, i32, z.batch), _status_at(dev_status, dev), _stream(stream)), "bass_paged_gather")
 
 
 def bass_paged_gather_int8(desc, Kpool, Vpool, K_codes, V_codes, K_scales, V_scales, tables, start, n, dev_status=None, stream=None):
-    torch, z = _torch(), _sizes_of(desc)
+    torch, z, dev = _torch(), _sizes_of(desc), _current()
     i8, f32, i32 = torch.int8, torch.float32, torch.int32
     _check(lib().bass_paged_gather_int8(
-        ctypes.byref(desc), _bytes_of(Kpool, z.pool, "Kpool"), _bytes_of(Vpool, z.pool, "Vpool"), _dev(K_codes, "K_codes", i8, z.rows),
-        _dev(V_codes, "V_codes", i8, z.rows), _dev(K_scales, "K_scales", f32, z.rows[:3]), _dev(V_scales, "V_scales", f32, z.rows[:3]),
-        _dev(tables, "tables", i32, z.tables), _dev(start, "start", i32, z.batch), _dev(n, "n", i32, z.batch),
-        _dev(dev_status, "dev_status", i32, optional=True),
-        _launch_on(stream, Kpool, Vpool, K_codes, V_codes, K_scales, V_scales, tables, start, n, dev_status)), "bass_paged_gather_int8")
+        ctypes.byref(desc), _bytes_of(Kpool, z.pool, "Kpool", dev), _bytes_of(Vpool, z.pool, "Vpool", dev), _at(K_codes, "K_codes", dev, i8, z.rows),
+        _at(V_codes, "V_codes", dev, i8, z.rows), _at(K_scales, "K_scales", dev, f32, z.rows[:3]), _at(V_scales, "V_scales", dev, f32, z.rows[:3]),
+        _at(tables, "tables", dev, i32, z.tables), _at(start, "start", dev, i32, z.batch), _at(n, "n", dev, i32, z.batch),
+        _status_at(dev_status, dev), _stream(stream)), "bass_paged_gather_int8")
 
 
 def bass_paged_attention_plan(desc, ctx_len, draft_len, prefix_of, prefix_len, plan, dev_status=None, stream=None):
     """prefix_of [B] (negative: none) and prefix_len [n_prefixes], or None for both: nothing is shared."""
-    i32, z = _torch().int32, _sizes_of(desc)
+    i32, z, dev = _torch().int32, _sizes_of(desc), _current()
     if (prefix_of is None) != (prefix_len is None):
         raise ValueError("prefix_of and prefix_len go together")
     if prefix_len is not None and (prefix_len.dim() != 1 or prefix_len.shape[0] == 0):
         raise ValueError("prefix_len must be [n_prefixes]")
     _check(lib().bass_paged_attention_plan(
-        ctypes.byref(desc), _dev(ctx_len, "ctx_len", i32, z.batch), _dev(draft_len, "draft_len", i32, z.batch),
-        _dev(prefix_of, "prefix_of", i32, z.batch, optional=True), _dev(prefix_len, "prefix_len", i32, optional=True),
-        0 if prefix_len is None else prefix_len.shape[0], _bytes_of(plan, z.plan, "plan"), plan.nbytes,
-        _dev(dev_status, "dev_status", i32, optional=True),
-        _launch_on(stream, plan, ctx_len, draft_len, prefix_of, prefix_len, dev_status)), "bass_paged_attention_plan")
+        ctypes.byref(desc), _at(ctx_len, "ctx_len", dev, i32, z.batch), _at(draft_len, "draft_len", dev, i32, z.batch),
+        _at_or_none(prefix_of, "prefix_of", dev, i32, z.batch), _at_or_none(prefix_len, "prefix_len", dev, i32),
+        0 if prefix_len is None else prefix_len.shape[0], _bytes_of(plan, z.plan, "plan", dev), plan.nbytes, _status_at(dev_status, dev),
+        _stream(stream)), "bass_paged_attention_plan")
 
 
 def bass_paged_verify_attention(desc, Q, Kpool, Vpool, tables, plan, O, lse, workspace, dev_status=None, stream=None):
-    torch, z = _torch(), _sizes_of(desc)
-    bf16, i32 = torch.bfloat16, torch.int32
+    torch, z, dev = _torch(), _sizes_of(desc), _current()
+    bf16 = torch.bfloat16
     _check(lib().bass_paged_verify_attention(
-        ctypes.byref(desc), _dev(Q, "Q", bf16, z.q), _bytes_of(Kpool, z.pool, "Kpool"), _bytes_of(Vpool, z.pool, "Vpool"),
-        _dev(tables, "tables", i32, z.tables), _bytes_of(plan, z.plan, "plan"), _dev(O, "O", bf16, z.q),
-        _dev(lse, "lse", torch.float32, z.lse, optional=True), _bytes_of(workspace, 0, "workspace"), workspace.nbytes,
-        _dev(dev_status, "dev_status", i32, optional=True),
-        _launch_on(stream, Q, Kpool, Vpool, tables, plan, O, lse, workspace, dev_status)), "bass_paged_verify_attention")
+        ctypes.byref(desc), _at(Q, "Q", dev, bf16, z.q), _bytes_of(Kpool, z.pool, "Kpool", dev), _bytes_of(Vpool, z.pool, "Vpool", dev),
+        _at(tables, "tables", dev, torch.int32, z.tables), _bytes_of(plan, z.plan, "plan", dev), _at(O, "O", dev, bf16, z.q),
+        _at_or_none(lse, "lse", dev, torch.float32, z.lse), _bytes_of(workspace, 0, "workspace", dev), workspace.nbytes,
+        _status_at(dev_status, dev), _stream(stream)), "bass_paged_verify_attention")
 
 
 # ---- allocation helpers (plumbing; no arithmetic) ----------------------------------------------

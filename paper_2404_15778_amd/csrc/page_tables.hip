@@ -346,6 +346,8 @@ extern "C" int bass_page_tables(int32_t rows, int32_t max_pages, int32_t page_to
   if (page_tokens % kBlockTokens != 0 || kmax > 65535) return BASS_ERR_UNSUPPORTED;
   if ((int64_t)rows * max_pages >= (1ll << 31) || (int64_t)n_pages * page_tokens >= (1ll << 31) || (int64_t)max_pages * page_tokens >= (1ll << 31))
     return BASS_ERR_UNSUPPORTED;
+  const int64_t slot_groups = ((int64_t)rows * kmax + 255) / 256;
+  if (slot_groups > 0x7fffffff) return BASS_ERR_UNSUPPORTED;
   if (workspace_bytes < bass_page_tables_workspace_bytes(rows, n_pages)) return BASS_ERR_WORKSPACE_TOO_SMALL;
   int32_t* ws = (int32_t*)workspace;
   const int tiles = tiles_of(n_pages);
@@ -360,9 +362,6 @@ extern "C" int bass_page_tables(int32_t rows, int32_t max_pages, int32_t page_to
   hipLaunchKernelGGL(page_rows, dim3(row_groups), dim3(256), 0, s, p);
   hipLaunchKernelGGL(page_counts, dim3(tiles + 1), dim3(kTileThreads), 0, s, p);
   hipLaunchKernelGGL(page_assign, dim3(tiles + row_groups), dim3(kTileThreads), 0, s, p);
-  if (slots && kmax > kInlineSlots) {
-    const int64_t groups = ((int64_t)rows * kmax + 255) / 256;
-    hipLaunchKernelGGL(page_slots, dim3((unsigned)groups), dim3(256), 0, s, p);
-  }
+  if (slots && kmax > kInlineSlots) hipLaunchKernelGGL(page_slots, dim3((unsigned)slot_groups), dim3(256), 0, s, p);
   return launch_status();
 }

@@ -68,17 +68,29 @@ __device__ inline PagedSegment paged_segment(const PagedRun& r, int unit, int of
 
 __device__ inline int row_of(const PagedParams& p, int r) { return (int)(((unsigned)r * p.g_magic) >> 20); }  // query token of a tile's row
 
-// Query token of a tile's row (any for a row that does not exist), as a row of [B * kmax].
-__device__ inline int token_of(const PagedParams& p, const PagedSegment& s, int row) {
-  const int t = row_of(p, row), at = s.tok + (t < s.n_tok ? t : 0);
-  return s.run.L < 0 ? p.tokens[at] : at;
+// Query tokens of a lane's rows (any for a row that does not exist), as rows of [B * kmax].  Requested in front of everything else: in a shared run the
+// queries wait for them.
+template <int NT>
+struct QueryTokens {
+  int tok[NT];
+};
+template <int NT>
+__device__ inline QueryTokens<NT> query_tokens(const PagedParams& p, const PagedSegment& s, int row0) {
+  QueryTokens<NT> q;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int t = row_of(p, row0 + 32 * nt), at = s.tok + (t < s.n_tok ? t : 0);
+    q.tok[nt] = s.run.L < 0 ? p.tokens[at] : at;
+  }
+  return q;
 }
 
 // Operand B of the score tiles.  A lane's row is c of each tile, and its two lanes (h) have the row's 16-byte chunks in turn.  A negative softmax
 // scale is moved into the queries (exact), and so is a zero; the factor that is left is positive.  INT8: quantized per row, with 127 (1 / amax) for the
 // cached rows' 127 / amax: the codes are the same but where x 127 / amax is a half to within its roundings.
 template <int D, bool kI8, int NT>
-__device__ inline void load_paged_queries(const PagedParams& p, const PagedSegment& s, int kvh, int c, int h, WideQueries<D, kI8, NT>& q) {
+__device__ inline void load_paged_queries(const PagedParams& p, const PagedSegment& s, const QueryTokens<NT>& tokens, int kvh, int c, int h,
+                                          WideQueries<D, kI8, NT>& q) {
   using G = Wide<D, kI8, NT>;
   const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
 #pragma unroll
@@ -86,7 +98,7 @@ __device__ inline void load_paged_queries(const PagedParams& p, const PagedSegme
     const int row = 32 * nt + c, t = row_of(p, row);
     const bool live = t < s.n_tok && p.scale_log2 != 0.f;
     const int hg = row - t * p.g;
-    const u32x4* src = (const u32x4*)(p.Q + ((size_t)token_of(p, s, row) * p.Hq + kvh * p.g + hg) * D);
+    const u32x4* src = (const u32x4*)(p.Q + ((size_t)tokens.tok[nt] * p.Hq + kvh * p.g + hg) * D);
     q.lim[nt] = s.run.L < 0 ? 0x7fffffff : s.run.L + (t < s.n_tok ? t : 0);
     const uint32_t keep = live ? 0xFFFFFFFFu : 0u;
     if constexpr (kI8) {
@@ -156,6 +168,7 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
     }
     return page * p.blocks_per_page + (blk - at * p.blocks_per_page);
   };
+  const QueryTokens<NT> tokens = query_tokens<NT>(p, s, c);
   PageWindow win{0, pool_blocks(0), 0};
   const int k_lane = 16 * G::k_lane(lane), v_lane = 16 * G::v_lane(lane);
   // One past the end goes through a buffer descriptor of size zero and touches nothing: all fetches are unconditional (exact wait counts).
@@ -182,7 +195,7 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
     fetch_v(ring[x], x);
   }
   WideQueries<D, kI8, NT> q;
-  load_paged_queries<D, kI8, NT>(p, s, kvh, c, h, q);
+  load_paged_queries<D, kI8, NT>(p, s, tokens, kvh, c, h, q);
   WideState<D, kI8, NT> st;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -346,6 +359,9 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
     const int blk = block_of_lane(t0);
     return (page * p.Hkv + s.kvh) * p.blocks_per_page + (blk - blk / p.blocks_per_page * p.blocks_per_page);
   };
+  // This wavefront's rows: from row 32 NT wv of the tile on.  Rows that do not exist have zero queries and are not stored.
+  const int row0 = 32 * NT * wv, rows = s.n_tok * p.g;
+  const QueryTokens<NT> tokens = query_tokens<NT>(p, s, row0 + c);
   int now = arrived(request(0), 0);  // lane l: block 64 w + l of window w
   // Whole rounds of 256 chunks (INT8 heads of 64: half of the threads have one).
   constexpr bool kHalf = kVec < 256;
@@ -387,10 +403,8 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   fetch_k(k_even, block_of(0));
   fetch_k(k_odd, block_of(1));
   fetch(v_even, p.Vp, block_of(0));
-  // This wavefront's rows: from row 32 NT wv of the tile on.  Rows that do not exist have zero queries and are not stored.
-  const int row0 = 32 * NT * wv, rows = s.n_tok * p.g;
   WideQueries<D, kI8, NT> q;
-  load_paged_queries<D, kI8, NT>(p, s, s.kvh, row0 + c, h, q);
+  load_paged_queries<D, kI8, NT>(p, s, tokens, s.kvh, row0 + c, h, q);
   // The queries stay in accumulation registers, where matrix instructions take an operand from as they are: the others' room is needed.
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)

@@ -140,7 +140,7 @@ inline int check_paged_attention(const bass_paged_desc* d) {
   if (d->B > kMaxPagedBatch || (int64_t)d->kmax * (d->Hq / d->Hkv) > 64) return BASS_ERR_UNSUPPORTED;
   // the list counts in 32 bits: every sequence's blocks, and at most as many again of shared runs
   const int64_t blocks = (int64_t)d->max_pages * (d->page_tokens / kBlockTokens);
-  if (((kCostRows2 + 3 * kCostTile2Int8) * blocks + kPadRows + kPadTile) * d->B * d->Hkv >= (1ll << 31) || 2 * (int64_t)d->B * d->kmax * d->Hq >= (1ll << 31)) return BASS_ERR_UNSUPPORTED;
+  if (((kCostRows2 + 3 * kCostTile2Int8 + 1) * blocks + kPadRows + kPadTile) * d->B * d->Hkv >= (1ll << 31) || 2 * (int64_t)d->B * d->kmax * d->Hq >= (1ll << 31)) return BASS_ERR_UNSUPPORTED;
   return BASS_OK;
 }
 
