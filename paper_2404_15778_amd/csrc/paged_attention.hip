@@ -491,7 +491,7 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   // [scores of B, block t + 1; values of B, block t | probabilities of A, block t + 1].  Operands are read from LDS eight matrix instructions ahead, V in
   // the first half and K in the second, behind their last use.  The last turn's scores are of the last block again, and their probabilities are not counted.
   // A wavefront has its SIMD for itself: what is to run beside a matrix instruction has to stand right behind it, and the compiler, left to
-  // itself, gathers the matrix instructions and lets the rest wait (200 instead of .. us).
+  // itself, gathers the matrix instructions and lets the rest wait (a prefix of 16 384 tokens, 64 sequences of 8 tokens, 32/8 heads of 128: 189 instead of 169 us).
   constexpr int kHalf16 = kSteps + kFrags;  // matrix instructions of a half turn
   int v_blk = 0;                            // block t + 3
   auto half_turn = [&](auto tile_m, auto tile_s, int t, int t_soft, bool counts, auto beside) {

@@ -255,6 +255,31 @@ def test_every_way_of_sharing(hip, dtype, D, n, q, Hq, Hkv, P):
     assert batch.shared_runs(pg) == 1
 
 
+def heads_per_unit(pg):
+    """kv heads of a unit where each workgroup of the plan starts (64 bytes of header; 32 bytes and the run of 64 bytes per workgroup)."""
+    shares = pg.plan[64:64 + 256 * 96].cpu().numpy().view(np.int32).reshape(256, 24)
+    return shares[shares[:, 4] > 0][:, 8 + 13]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "int8kv"])
+@pytest.mark.parametrize("B,kmax,Hq,Hkv,D,most", [(64, 4, 10, 5, 64, 252), (64, 4, 10, 5, 128, 252), (64, 8, 40, 5, 128, 500), (64, 8, 40, 5, 64, 500),
+                                                  (200, 3, 6, 2, 128, 200), (300, 1, 4, 4, 64, 511)])
+@pytest.mark.parametrize("shared", [False, True])
+def test_many_short_sequences(hip, dtype, B, kmax, Hq, Hkv, D, most, shared):
+    """A wavefront per kv head: heads that do not fill the workgroup's four, up to 32 query rows and more, whole units and cut ones, sequences
+    alone and the rests of a prefix's."""
+    rng = np.random.default_rng([B, Hq, D])
+    ctx, nq = rng.integers(0, most - kmax, size=B), rng.integers(0, kmax + 1, size=B)
+    nq[:3] = kmax
+    of = np.where(np.arange(B) % 3 == 0, 0, -1) if shared else None
+    if shared:
+        ctx = ctx + 1024 * (of == 0)
+    batch = Batch(B + D, Hq, Hkv, D, 32, ctx, nq, kmax, of, [1024] if shared else None, dtype)
+    pg = batch.pages(hip)
+    batch.check(hip, pg=pg)
+    assert (heads_per_unit(pg) == 4).any()
+
+
 def test_the_same_call_gives_the_same_bits(hip):
     """Nothing depends on the order in which workgroups arrive.  (Equal sequences agree up to rounding only: the list is cut at other blocks of each.)"""
     n = 24
