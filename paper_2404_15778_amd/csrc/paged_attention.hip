@@ -441,11 +441,20 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   auto value = [&](int nt, int x) {
     acc[nt][x >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[x]), pf[nt][x & 1], acc[nt][x >> 1], 0, 0, 0);
   };
+  // INT8: scales of a lane's 16 tokens, of K of block t + 1 and of V, read ahead of their use as the operands are.
+  float ks[kI8 ? 16 : 1], vs[kI8 ? 16 : 1];
+  auto read_scales = [&](float* to, int y, int t, int first) {
+    if constexpr (kI8) {
+      const f32x4 four = *(const f32x4*)&lds.scales[t & 3][first + G::token(4 * y, h)];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[4 * y + i] = four[i];
+    }
+  };
   // Softmax of a tile of rows, element by element (16 of a lane), so that it can be laid between matrix instructions.
   float mx[NT], sum[NT], m_use[NT], arg[NT][16];
-  // Score i of block t as a number.  INT8: times the scales of token and row, multiplied first.
-  auto take = [&](int nt, int i, int t) {
-    if constexpr (kI8) e[nt][i] = (float)z[nt][i] * (lds.scales[t & 3][G::token(i, h)] * q.row_scale[nt]);
+  // Score i as a number.  INT8: times the scales of token and row, multiplied first.
+  auto take = [&](int nt, int i) {
+    if constexpr (kI8) e[nt][i] = (float)z[nt][i] * (ks[i] * q.row_scale[nt]);
     else e[nt][i] = z[nt][i];
     mx[nt] = i == 0 ? e[nt][0] : fmaxf(mx[nt], e[nt][i]);
   };
@@ -465,7 +474,7 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
     sum[nt] = 0.f;
   };
   // Probability i in three steps, one behind the other: argument, exponential, sum and operand.
-  auto soft = [&](int nt, int i, int t) {
+  auto soft = [&](int nt, int i) {
     if (i < 16) arg[nt][i] = kI8 ? e[nt][i] - m_use[nt] : (e[nt][i] - m_use[nt]) * factor;
     if (i >= 1 && i < 17) e[nt][i - 1] = __builtin_amdgcn_exp2f(arg[nt][i - 1]);
     if (i >= 2 && i < 18) {
@@ -473,8 +482,8 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
       sum[nt] += e[nt][j];
       if (j & 1) {
         if constexpr (kI8) {
-          pf[nt][j >> 3][(j & 7) - 1] = (__bf16)(e[nt][j - 1] * lds.scales[t & 3][32 + G::token(j - 1, h)]);
-          pf[nt][j >> 3][j & 7] = (__bf16)(e[nt][j] * lds.scales[t & 3][32 + G::token(j, h)]);
+          pf[nt][j >> 3][(j & 7) - 1] = (__bf16)(e[nt][j - 1] * vs[j - 1]);
+          pf[nt][j >> 3][j & 7] = (__bf16)(e[nt][j] * vs[j]);
         } else {
           pf[nt][j >> 3][(j & 7) - 1] = (__bf16)e[nt][j - 1];
           pf[nt][j >> 3][j & 7] = (__bf16)e[nt][j];
@@ -494,19 +503,19 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   // itself, gathers the matrix instructions and lets the rest wait (a prefix of 16 384 tokens, 64 sequences of 8 tokens, 32/8 heads of 128: 189 instead of 169 us).
   constexpr int kHalf16 = kSteps + kFrags;  // matrix instructions of a half turn
   int v_blk = 0;                            // block t + 3
-  auto half_turn = [&](auto tile_m, auto tile_s, int t, int t_soft, bool counts, auto beside) {
+  auto half_turn = [&](auto tile_m, auto tile_s, bool counts, auto beside) {
     constexpr int nm = decltype(tile_m)::value, ns = decltype(tile_s)::value;
 #pragma unroll
     for (int x = 0; x < kHalf16; ++x) {
       if (x < kSteps) score(nm, x);
       else value(nm, x - kSteps);
 #pragma unroll
-      for (int i = x * 18 / kHalf16; i < (x + 1) * 18 / kHalf16; ++i) soft(ns, i, t_soft);
+      for (int i = x * 18 / kHalf16; i < (x + 1) * 18 / kHalf16; ++i) soft(ns, i);
       if (x > kSteps) {
         constexpr int n = kFrags - 1;
         const int y = x - kSteps - 1;
 #pragma unroll
-        for (int i = y * 16 / n; i < (y + 1) * 16 / n; ++i) take(nm, i, t + 1);
+        for (int i = y * 16 / n; i < (y + 1) * 16 / n; ++i) take(nm, i);
       }
       beside(x);
       __builtin_amdgcn_sched_barrier(0);
@@ -518,15 +527,20 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
     const bool more = t + 1 < s.n;
     const int k_blk = block_of(t + 4);
     if constexpr (NT == 2) {
-      half_turn(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{}, t, t, true, [&](int x) {
+      half_turn(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{}, true, [&](int x) {
         if (x < kFrags) read_v(x, t);
+        if (x < 4) read_scales(ks, x, t + 1, 0);
         if (x == 1) commit_k(k_stage, t + 2);
         if (x == 2) commit_v(v_stage, t + 1);
         if (x == 4) fetch_k(k_stage, k_blk);
         if (x == 5) fetch(v_stage, p.Vp, v_blk);
       });
       __syncthreads();
-      half_turn(std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{}, t, t + 1, more, [&](int x) {
+      half_turn(std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{}, more, [&](int x) {
+        if (x == 0) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y) read_scales(vs, y, t + 1, 32);
+        }
         if (x < kSteps) read_k(x, t + 2);
       });
     } else {
@@ -535,6 +549,11 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
       fetch_k(k_stage, k_blk);
       fetch(v_stage, p.Vp, v_blk);
       __syncthreads();
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        read_scales(ks, y, t + 1, 0);
+        read_scales(vs, y, t + 1, 32);
+      }
 #pragma unroll
       for (int x = 0; x < kSteps; ++x) {
         score(0, x);
@@ -546,10 +565,10 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
         read_v(x, t + 1);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) take(0, i, t + 1);
+      for (int i = 0; i < 16; ++i) take(0, i);
       settle(0);
 #pragma unroll
-      for (int i = 0; i < 18; ++i) soft(0, i, t + 1);
+      for (int i = 0; i < 18; ++i) soft(0, i);
       finish(0, more);
     }
     v_blk = k_blk;
@@ -575,13 +594,18 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
     for (int x = 0; x < kFrags; ++x) read_v(x, 0);
   }
 #pragma unroll
+  for (int y = 0; y < 4; ++y) {
+    read_scales(ks, y, 0, 0);
+    read_scales(vs, y, 0, 32);
+  }
+#pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) take(nt, i, 0);
+    for (int i = 0; i < 16; ++i) take(nt, i);
     settle(nt);
   }
 #pragma unroll
-  for (int i = 0; i < 18; ++i) soft(0, i, 0);
+  for (int i = 0; i < 18; ++i) soft(0, i);
   finish(0, true);
   __syncthreads();  // before the first turn writes over block 0
   // Windows of 64 blocks: turn t asks for block t + 4.  The inner loop has no loads but those of the stages and no way out between its two

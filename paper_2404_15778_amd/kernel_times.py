@@ -22,7 +22,7 @@ flat rows (1.0 / 0.9) and the plain softmax (1.0 / 1.0) -- or at the one setting
 setting, bass_spec_accept on the rows made and bass_warp_accept on the logits (drafts: the draft model's
 most likely tokens).
 
-`case` prepares a listed case of perf/cases.py (seed 1), launches one small bass_bench_stream_read as a marker and runs the
+`case` prepares a listed case of perf/cases.py or perf/operators.py (seed 1), launches one small bass_bench_stream_read as a marker and runs the
 case --passes times; `summarize --after-marker` leaves out everything up to that marker.
 
 Needs the GPU and the built library (except `summarize`).
@@ -148,10 +148,17 @@ def case(args):
     import paper_2404_15778_amd as bass
 
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-    spec = importlib.util.spec_from_file_location("cases", os.path.join(root, "perf", "cases.py"))
-    cases = importlib.util.module_from_spec(spec)
-    spec.loader.exec_module(cases)
-    state = cases.prepare(next(c for c in cases.listed() if c["name"] == args.name), 1)
+    for file in ("cases", "operators"):
+        spec = importlib.util.spec_from_file_location(file, os.path.join(root, "perf", file + ".py"))
+        cases = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(cases)
+        found = [c for c in cases.listed() if c["name"] == args.name]
+        if found:
+            break
+    else:
+        raise SystemExit(f"no case {args.name}")
+    cases.own = True
+    state = cases.prepare(found[0], 1)
     kv = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda:0")
     bass.bass_bench_stream_read(kv, kv, kv.numel(), 4)
     for _ in range(args.passes):
