@@ -348,6 +348,8 @@ size_t bass_page_pool_bytes(const bass_paged_desc* desc);
  * and all rows behind it that need any, take none (BASS_STATUS_NO_PAGES): their tables stay valid for what they hold.
  * Lengths below 0 or over max_pages * page_tokens are clamped, n_new to [0, kmax] (BASS_STATUS_LEN_CLAMPED); a share_from that is no row or the
  * row itself shares nothing (BASS_STATUS_LEN_CLAMPED).  Entries that are no page are neither shared nor counted (BASS_STATUS_PAGE_CLAMPED).
+ * Pages that several rows hold are not copied when one of them is written: a row appends behind what it shares, and one that has to go back into it
+ * gives all its pages back first (length 0) and begins again.
  * The result does not depend on the order in which anything runs.  rows, max_pages, n_pages > 0, page_tokens a multiple of 32, rows * max_pages < 2^31,
  * n_pages * page_tokens < 2^31, 0 <= kmax <= 65535.  workspace: device, 16-byte aligned, at least bass_page_tables_workspace_bytes(rows, n_pages) bytes,
  * contents irrelevant on entry.  One launch for few rows of a small pool, else three or four.
@@ -386,7 +388,8 @@ int bass_paged_gather_int8(const bass_paged_desc* desc, const void* Kpool, const
  *   ctx_len, draft_len [B]    as in bass_verify_attention; ctx_len + draft_len <= max_pages * page_tokens (else clamped, BASS_STATUS_LEN_CLAMPED)
  *   prefix_of [B] or NULL     number of the prefix a sequence begins with, negative: none
  *   prefix_len [n_prefixes]   tokens of each prefix; n_prefixes <= 4096, 0 if prefix_of is NULL
- * The tables of sequences with the same prefix must name the same pages for its tokens, as bass_page_tables makes them.  What is
+ * The tables of sequences with the same prefix must name the same pages for its tokens, as bass_page_tables makes them where prefix_len is what it
+ * shared (share_len down to whole pages), or pages that hold the same rows: those of the first of them with query tokens are read.  What is
  * common to all of a prefix's sequences in this step (at most the shortest one's ctx_len, whole blocks of 32 tokens) is computed for all of
  * them together where that is quicker; the result is that of separate sequences up to rounding.  Numbers outside [0, n_prefixes) count as none (from
  * n_prefixes on with BASS_STATUS_LEN_CLAMPED).

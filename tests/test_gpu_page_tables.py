@@ -63,6 +63,19 @@ def test_random_calls(hip, rows, most, P, pages, kmax):
     assert not seen & ~(NO_PAGES | 1)
 
 
+def test_more_rows_than_are_kept_in_lds(hip):
+    """5000 rows, three calls; some share, some end, and some find no pages."""
+    rng = random.Random(5)
+    rows, most, P, pages = 5000, 3, 32, 4501
+    both, seen = Both(hip, rows, most, P, pages), 0
+    for _ in range(3):
+        length = [rng.choice((0, rng.randint(1, most * P))) for _ in range(rows)]
+        sf = [rng.choice((-1, rng.randrange(rows))) for _ in range(rows)]
+        sf = [-1 if x == r else x for r, x in enumerate(sf)]
+        seen |= both.update(length, sf, [rng.randint(0, most * P) for _ in range(rows)], [max(n - 2, 0) for n in length], [min(n, 2) for n in length], 3)
+    assert seen == NO_PAGES
+
+
 def test_slots_far_beyond_two_to_the_thirty(hip):
     """Page numbers whose slots need all 31 bits."""
     P, pages = 1 << 20, 2047

@@ -157,6 +157,17 @@ def test_prefix_longer_than_some_sequences(hip):
     batch.check(hip)
 
 
+@pytest.mark.parametrize("n", [3, 20])
+def test_prefix_that_ends_inside_a_page(hip, n):
+    """Whole pages are shared; the rest of the prefix lies in pages of each sequence's own, which hold the same rows."""
+    P, common = 96, 20 * 96 + 71
+    batch = Batch(13, 32, 8, 128, P, common + np.arange(n) * 7, [3] * n, 4, np.zeros(n, int), [common])
+    batch.K[:, :common], batch.V[:, :common] = batch.K[0, :common], batch.V[0, :common]
+    pg = batch.pages(hip)
+    batch.check(hip, pg=pg)
+    assert batch.shared_runs(pg) == (1 if n == 20 else 0)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 3.0])
 def test_scales(hip, scale):
     """Products of at most 64 together: |scale| sum |q k| < 3 * 3 * 3 ... is not bounded so for scale 3, so inputs are an eighth."""
