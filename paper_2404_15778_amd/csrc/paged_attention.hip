@@ -368,15 +368,19 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   // This wavefront's rows: from row 32 NT wv of the tile on.  Rows that do not exist have zero queries and are not stored.
   const int row0 = 32 * NT * wv, rows = s.n_tok * p.g;
   const QueryTokens<NT> tokens = query_tokens<NT>(p, s, row0 + c);
-  int now = arrived(request(0), 0);  // lane l: block 64 w + l of window w
+  // Blocks on their way in registers, of K and of V.  Two cover the way from memory, but for bf16 blocks under 128 rows: a workgroup wants 16 KB in 0.6 us
+  // there (a prompt of 32 768 tokens, 16 sequences of 6, 32 heads: 114 instead of 120 us with four; INT8 115 either way).
+  constexpr int S = NT == 1 && !kI8 ? 4 : 2, kAhead = 2 + S;  // turn t asks for block t + kAhead of K and for the one before it of V
+  const int start_blocks = arrived(request(0), 0);    // lane l: block l
+  int now = arrived(request(kAhead), kAhead);         // lane l: the block that turn 64 w + l asks for
   // Whole rounds of 256 chunks (INT8 heads of 64: half of the threads have one).
   constexpr bool kHalf = kVec < 256;
   const int mine = kHalf ? tid & (kVec - 1) : tid;
   struct Stage {
     u32x4 a, b;
     float scale;
-  } k_even, k_odd, v_even, v_odd;
-  auto block_of = [&](int t) { return __builtin_amdgcn_readlane(now, t & 63); };
+  } k0, k1, k2, k3, v0, v1, v2, v3;
+  auto start_block = [&](int t) { return __builtin_amdgcn_readlane(start_blocks, t); };
   auto fetch = [&](Stage& r, const uint4* pool, int blk) {
     const u32x4* at = (const u32x4*)(pool + (size_t)blk * kPool) + mine;
     r.a = at[0];
@@ -406,9 +410,9 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
       if constexpr (kLoads == 2) to[256 + mine] = r.b;
     }
   };
-  fetch_k(k_even, block_of(0));
-  fetch_k(k_odd, block_of(1));
-  fetch(v_even, p.Vp, block_of(0));
+  fetch_k(k0, start_block(0));
+  fetch_k(k1, start_block(1));
+  fetch(v0, p.Vp, start_block(0));
   WideQueries<D, kI8, NT> q;
   load_paged_queries<D, kI8, NT>(p, s, tokens, s.kvh, row0 + c, h, q);
   // The queries stay in accumulation registers, where matrix instructions take an operand from as they are: the others' room is needed.
@@ -508,7 +512,7 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
   // A wavefront has its SIMD for itself: what is to run beside a matrix instruction has to stand right behind it, and the compiler, left to
   // itself, gathers the matrix instructions and lets the rest wait (a prefix of 16 384 tokens, 64 sequences of 8 tokens, 32/8 heads of 128: 189 instead of 169 us).
   constexpr int kHalf16 = kSteps + kFrags;  // matrix instructions of a half turn
-  int v_blk = 0;                            // block t + 3
+  int v_blk = 0;                            // block t + kAhead - 1
   auto half_turn = [&](auto tile_m, auto tile_s, bool counts, auto beside) {
     constexpr int nm = decltype(tile_m)::value, ns = decltype(tile_s)::value;
 #pragma unroll
@@ -530,8 +534,7 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
     settle(nm);
   };
   auto turn = [&](int t, Stage& k_stage, Stage& v_stage) {
-    const bool more = t + 1 < s.n;
-    const int k_blk = block_of(t + 4);
+    const int k_blk = __builtin_amdgcn_readlane(now, t & 63);
     if constexpr (NT == 2) {
       half_turn(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{}, true, [&](int x) {
         if (x < kFrags) read_v(x, t);
@@ -542,7 +545,7 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
         if (x == 5) fetch(v_stage, p.Vp, v_blk);
       });
       __syncthreads();
-      half_turn(std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{}, more, [&](int x) {
+      half_turn(std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{}, t + 1 < s.n, [&](int x) {
         if (x == 0) {
 #pragma unroll
           for (int y = 0; y < 4; ++y) read_scales(vs, y, t + 1, 32);
@@ -550,43 +553,57 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
         if (x < kSteps) read_k(x, t + 2);
       });
     } else {
-      commit_k(k_stage, t + 2);
-      commit_v(v_stage, t + 1);
-      fetch_k(k_stage, k_blk);
-      fetch(v_stage, p.Vp, v_blk);
-      __syncthreads();
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        read_scales(ks, y, t + 1, 0);
-        read_scales(vs, y, t + 1, 32);
-      }
 #pragma unroll
       for (int x = 0; x < kSteps; ++x) {
         score(0, x);
-        read_k(x, t + 2);
+#pragma unroll
+        for (int i = x * 18 / kSteps; i < (x + 1) * 18 / kSteps; ++i) soft(0, i);
+#pragma unroll
+        for (int i = x * kFrags / kSteps; i < (x + 1) * kFrags / kSteps; ++i) read_v(i, t);
+        if (x == 0) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y) read_scales(ks, y, t + 1, 0);
+          commit_k(k_stage, t + 2);
+          fetch_k(k_stage, k_blk);
+        }
+        if (x == 1) {
+          commit_v(v_stage, t + 1);
+          fetch(v_stage, p.Vp, v_blk);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
+      finish(0, true);
+      __syncthreads();
 #pragma unroll
       for (int x = 0; x < kFrags; ++x) {
         value(0, x);
-        read_v(x, t + 1);
+#pragma unroll
+        for (int i = x * 16 / kFrags; i < (x + 1) * 16 / kFrags; ++i) take(0, i);
+        if (x == 0) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y) read_scales(vs, y, t + 1, 32);
+        }
+        if (x < kSteps) read_k(x, t + 2);
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) take(0, i);
       settle(0);
-#pragma unroll
-      for (int i = 0; i < 18; ++i) soft(0, i);
-      finish(0, more);
     }
     v_blk = k_blk;
   };
-  commit_k(k_even, 0);
-  commit_k(k_odd, 1);
-  commit_v(v_even, 0);
-  fetch_k(k_even, block_of(2));  // in the order of the turns: the wait counts of the loop's entry and of its end are the same
-  fetch(v_even, p.Vp, block_of(1));
-  fetch_k(k_odd, block_of(3));
-  fetch(v_odd, p.Vp, block_of(2));
-  v_blk = block_of(3);
+  commit_k(k0, 0);
+  commit_k(k1, 1);
+  commit_v(v0, 0);
+  fetch_k(k0, start_block(2));  // in the order of the turns: the wait counts of the loop's entry and of its end are the same
+  fetch(v0, p.Vp, start_block(1));
+  fetch_k(k1, start_block(3));
+  fetch(v1, p.Vp, start_block(2));
+  if constexpr (S == 4) {
+    fetch_k(k2, start_block(4));
+    fetch(v2, p.Vp, start_block(3));
+    fetch_k(k3, start_block(5));
+    fetch(v3, p.Vp, start_block(4));
+  }
+  v_blk = start_block(kAhead - 1);
   __syncthreads();
 #pragma unroll
   for (int x = 0; x < kSteps; ++x) {
@@ -594,10 +611,6 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) score(nt, x);
     read_k(x, 1);
-  }
-  if constexpr (NT == 1) {
-#pragma unroll
-    for (int x = 0; x < kFrags; ++x) read_v(x, 0);
   }
 #pragma unroll
   for (int y = 0; y < 4; ++y) {
@@ -610,23 +623,32 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
     for (int i = 0; i < 16; ++i) take(nt, i);
     settle(nt);
   }
+  if constexpr (NT == 2) {
 #pragma unroll
-  for (int i = 0; i < 18; ++i) soft(0, i);
-  finish(0, true);
+    for (int i = 0; i < 18; ++i) soft(0, i);
+    finish(0, true);
+  }
   __syncthreads();  // before the first turn writes over block 0
-  // Windows of 64 blocks: turn t asks for block t + 4.  The inner loop has no loads but those of the stages and no way out between its two
-  // turns, so that its wait counts are exact.
+  // Windows of 64 turns.  The inner loop has no loads but those of the stages and no way out between its S turns, so that its wait counts are exact.
   int t = 0;
-  for (int end = 60;; end += 64) {
-    const int page = request(end + 4);
-    for (const int stop = min(end, s.n) - 1; t < stop; t += 2) {
-      turn(t, k_even, v_even);
-      turn(t + 1, k_odd, v_odd);
+  for (int end = 64;; end += 64) {
+    const int page = request(end + kAhead);
+    for (const int stop = min(end, s.n) - (S - 1); t < stop; t += S) {
+      turn(t, k0, v0);
+      turn(t + 1, k1, v1);
+      if constexpr (S == 4) {
+        turn(t + 2, k2, v2);
+        turn(t + 3, k3, v3);
+      }
     }
     if (end >= s.n) break;
-    now = arrived(page, end + 4);
+    now = arrived(page, end + kAhead);
   }
-  if (t < s.n) turn(t, k_even, v_even);
+  if (t < s.n) turn(t, k0, v0);
+  if constexpr (S == 4) {
+    if (t + 1 < s.n) turn(t + 1, k1, v1);
+    if (t + 2 < s.n) turn(t + 2, k2, v2);
+  }
   if (bad && p.status) atomicOr(p.status, BASS_STATUS_PAGE_CLAMPED);
   const size_t base = partial_row(s.run, p.g, s.kvh, s.tile, wg);
 #pragma unroll

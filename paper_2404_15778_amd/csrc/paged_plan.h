@@ -18,8 +18,10 @@ constexpr int kPagedWaves = 4;      // wavefronts of a workgroup
 constexpr int kPagedShares = 256;   // workgroups of the attention launch: one per compute unit
 // An entry is 1/8 us.  Of a block: up to 32 and 64 rows (four blocks at a time, a wavefront each); tiles of 128 and 256 rows (a block at a time, all
 // wavefronts) over bf16 and INT8 pages.  Of the end of a unit, with the beginning of the next: by a wavefront per head, by all four, and of a tile.
-constexpr int kCostRows1 = 4, kCostRows2 = 6, kCostTile1 = 6, kCostTile2 = 8, kCostTile1Int8 = 9, kCostTile2Int8 = 13;
-constexpr int kPadHeads = 32, kPadRows = 40, kPadTile = 76;
+// Fitted to kernel times, us per layer before and with these: INT8, 6 sequences of 5 tokens behind 32 768, 32/8 heads 54 -> 35 (the workgroups without a tile had been given too
+// much); 16 sequences of 6 behind 8192, 32 heads 47 -> 41, over INT8 51 -> 39; 64 of 8 behind 16 384, 32/8 heads, INT8 222 -> 200; three prompts 46 -> 42.
+constexpr int kCostRows1 = 4, kCostRows2 = 6, kCostTile1 = 5, kCostTile2 = 7, kCostTile1Int8 = 5, kCostTile2Int8 = 10;
+constexpr int kPadHeads = 64, kPadRows = 56, kPadTile = 76;
 constexpr int kTileStart = 48;  // a workgroup that begins with a tile loses so much more than one that begins with few rows (see tile_cost)
 // Short runs give each wavefront a kv head of its own: nothing is merged, but a workgroup has four partial results, and the list has fewer, longer
 // units.  Worth it where units are many.  us per layer, heads of 128, 4 tokens, without -> with: 32/8 heads, 32 sequences of 40 / 100 / 200 / 400 tokens
@@ -62,12 +64,12 @@ BASS_HD inline int block_cost(bool shared, int rows, int heads, bool int8) {
 BASS_HD inline int unit_pad(bool shared, int rows, int heads) { return is_tile(shared, rows) ? kPadTile : heads > 1 ? kPadHeads : kPadRows; }
 // Whether a common prefix is computed for all of its sequences together.  Separate sequences read it again from the caches; together, a workgroup has one
 // more beginning and end, and every row one more partial result.  us per layer, separate / together, prefixes of 256 / 512 / 1024 / 2048 / 4096 tokens, 200
-// of their own, 4 query tokens: 32 heads, 2 sequences 13.1 / 13.8 / 14.3 / 16.9 / 22.8 and 13.8 / 14.1 / 14.4 / 17.1 / 22.1, 4 sequences 14.5 / 15.3 / 17.7 / 22.3 / 31.9 and 14.6 /
-// 14.5 / 15.5 / 19.3 / 24.2, 8 sequences 19.2 / 23.0 / 30.9 / 48.2 / 81.9 and 16.8 / 16.7 / 18.8 / 20.9 / 26.3; 32/8 heads, 8 sequences 13.6 / 14.8 / 16.0 / 20.2 / 28.0 and 14.9 / 16.6 / 19.7 /
-// 22.7 / 27.1, 32 sequences 22.2 / 26.0 / 33.6 / 51.9 / 89.2 and 26.1 / 27.9 / 29.2 / 34.2 / 37.4; 64/8 heads, 8 sequences 14.0 / 15.5 / 17.4 / 22.0 / 29.4 and 21.3 / 23.5 / 26.7 / 28.0 /
-// 32.9, 32 sequences 24.9 / 29.1 / 37.5 / 55.5 / 94.3 and 28.7 / 33.8 / 36.2 / 39.6 / 49.4.  In entries saved per workgroup: from about 20 on, or 100 with tiles, whose
+// of their own, 4 query tokens: 32 heads, 2 sequences 13.5 / 13.9 / 14.9 / 18.5 / 24.1 and 13.2 / 13.7 / 14.5 / 16.6 / 21.6, 4 sequences 13.8 / 16.0 / 18.6 / 23.1 / 32.8 and 13.7 /
+// 15.4 / 16.7 / 18.6 / 22.8, 8 sequences 19.2 / 23.2 / 31.4 / 49.2 / 83.2 and 16.3 / 16.5 / 18.0 / 20.1 / 25.5; 32/8 heads, 8 sequences 14.0 / 14.7 / 15.7 / 20.3 / 29.5 and 13.9 / 15.7 / 17.3 /
+// 20.4 / 24.0, 32 sequences 21.7 / 25.0 / 33.2 / 54.2 / 94.1 and 24.4 / 26.5 / 27.8 / 32.4 / 35.8; 64/8 heads, 8 sequences 14.6 / 15.5 / 17.0 / 21.7 / 31.4 and 18.8 / 21.9 / 25.9 / 27.1 /
+// 28.2, 32 sequences 24.1 / 27.8 / 36.2 / 58.7 / 98.1 and 26.1 / 27.3 / 33.6 / 37.5 / 45.1.  In entries saved per workgroup: from about 12 on, or 55 with tiles, whose
 // beginnings are long; but those are paid once for all prefixes of a batch.
-constexpr int kSavedRows = 20, kSavedTile = 100;
+constexpr int kSavedRows = 12, kSavedTile = 55;
 BASS_HD inline int saved_by_sharing(int members, int tokens, int tiles, int tile_tok, int n_blk, int g, int Hkv, bool int8) {
   const int64_t apart = (int64_t)members * block_cost(false, tokens * g / members, 1, int8), together = (int64_t)tiles * block_cost(true, tile_tok * g, 1, int8);
   const int64_t saved = (apart - together) * n_blk * Hkv / kPagedShares;
