@@ -12,9 +12,10 @@
 //
 // us per layer, attention + merge.  Few rows: bound by the trips to memory of a launch, one behind the other (8 answers of up to 7 tokens to a prompt of 1500, 32 heads:
 // 14 + 4 for 37 MB), and in long contexts by memory (16 sequences of up to 8192 tokens: 21 + 4 for 88 MB, 4.2 TB/s).  Tiles: 3 prefixes of up to 8000 tokens, 32
-// sequences of 5 tokens, 64/8 heads: 46 + 9 (16 GFLOP; every workgroup has but a few blocks between the 6 us that a tile's beginning takes and the
+// sequences of 5 tokens, 64/8 heads: 42 + 7 (16 GFLOP; every workgroup has but a few blocks between the 6 us that a tile's beginning takes and the
 // 3 of its end); a prefix of 16 384, 64 sequences of 8, 32/8 heads: 160 - 180 + 11 (137 GFLOP, 0.8 PFLOP/s): issue of matrix and softmax instructions from one
-// wavefront per SIMD, at the clock that the card's power leaves.  INT8, a prefix of 4096, 24 sequences of one token, 64/8 heads: 28 + 6, the same bounds.
+// wavefront per SIMD, at the clock that the card's power leaves.  INT8, a prefix of 4096, 24 sequences of one token, 64/8 heads: 26 + 6, the same bounds.  Tiles of up to 128
+// rows: 16 sequences of 6 behind 32 768 tokens, 32 heads: 114 + 7 (555 MB, 4.9 TB/s).
 #include "paged_plan.h"
 #include "wide_tiles.h"
 
