@@ -382,6 +382,36 @@ def test_a_context_of_two_million_tokens(hip):
     assert int(pg.status.item()) == 0
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("int8kv", 128), ("int8kv", 64)])
+@pytest.mark.parametrize("n", [10, 40])
+@pytest.mark.parametrize("blocks", [2100, 4301])
+def test_long_stretches_of_a_shared_prefix(hip, dtype, D, n, blocks):
+    """65 and 134 blocks per workgroup and what lies around them, in tiles of 60 and of 240 query rows.  Keys are zero, so that lse counts the tokens; a
+    page's values are one whole number (O: probabilities, over INT8 pages times the scale, and O itself are rounded to bf16: 2^-8 each)."""
+    rng = np.random.default_rng([blocks, n])
+    Hq, Hkv, P, q, unique = 16, 8, 32, 3, 150
+    pages = unique + 2 * n
+    pg = hip.DevicePages(n, q, Hq, Hkv, D, P, pages, blocks + 2, dtype, 0.125)
+    value = rng.integers(-8, 9, size=pages)
+    V = np.repeat(value, P).astype(np.float32)[None, :, None, None] * np.ones((1, 1, Hkv, D), np.float32)
+    pg.append(hip.to_device(np.zeros(V.shape, np.uint16)), hip.to_device(wl.to_bf16_bits(V)), hip.i32(np.arange(pages * P)[None]))
+    prefix = rng.integers(0, unique, size=blocks)
+    own = unique + rng.permutation(2 * n).reshape(n, 2)
+    tables = np.concatenate([np.repeat(prefix[None], n, 0), own], 1)
+    extra = rng.integers(0, 40, size=n)
+    Q = wl.to_bf16_bits(rng.standard_normal((n, q, Hq, D), dtype=np.float32))
+    O, lse = pg.verify(hip.to_device(Q), hip.i32(tables), hip.i32(blocks * P + extra), hip.i32([q] * n), hip.i32([0] * n), hip.i32([blocks * P]))
+    assert int(pg.plan[:8].cpu().numpy().view(np.int32)[1]) == n + 1 and int(pg.status.item()) == 0
+    O, lse = wl.bf16_bits_to_f32(hip.to_host(O)), hip.to_host(lse)
+    for b in range(n):
+        for i in range(q):
+            tail = np.repeat(value[own[b]], P)[:extra[b] + i + 1]
+            count = blocks * P + len(tail)
+            mean, size = (P * value[prefix].sum() + tail.sum()) / count, (P * np.abs(value[prefix]).sum() + np.abs(tail).sum()) / count
+            assert np.abs(lse[b, i] - np.log(count)).max() <= 2e-6
+            assert np.abs(O[b, i] - mean).max() <= 2 ** -8 * abs(mean) + (2 ** -8 * size if dtype == "int8kv" else 1e-5)
+
+
 def test_replayed_graph(hip):
     """Plan and two layers captured; every replay, with other lengths and eager work between, equals the eager call bit for bit."""
     import torch
