@@ -20,8 +20,10 @@ constexpr int kPagedShares = 256;   // workgroups of the attention launch: one p
 // wavefronts) over bf16 and INT8 pages.  Of the end of a unit, with the beginning of the next: by a wavefront per head, by all four, and of a tile.
 // Fitted to kernel times, us per layer before and with these: INT8, 6 sequences of 5 tokens behind 32 768, 32/8 heads 54 -> 35 (the workgroups without a tile had been given too
 // much); 16 sequences of 6 behind 8192, 32 heads 47 -> 41, over INT8 51 -> 39; 64 of 8 behind 16 384, 32/8 heads, INT8 222 -> 200; three prompts 46 -> 42.
+// The end of a tile at 76 / 108: 16 sequences of 4 behind 4096, 32/8 heads 24.7 / 21.1, 32 of 4 behind 1024, 64/8 heads 26.9 / 24.4; 32 of 4 behind 512, 32 heads, with the merge 31.3 / 34.2, 8 behind
+// 4096, 64/8 heads, 28.3 / 30.5; the others level.
 constexpr int kCostRows1 = 4, kCostRows2 = 6, kCostTile1 = 5, kCostTile2 = 7, kCostTile1Int8 = 5, kCostTile2Int8 = 10;
-constexpr int kPadHeads = 64, kPadRows = 56, kPadTile = 76;
+constexpr int kPadHeads = 64, kPadRows = 56, kPadTile = 108;
 constexpr int kTileStart = 48;  // a workgroup that begins with a tile loses so much more than one that begins with few rows (see tile_cost)
 // Short runs give each wavefront a kv head of its own: nothing is merged, but a workgroup has four partial results, and the list has fewer, longer
 // units.  Worth it where units are many.  us per layer, heads of 128, 4 tokens, without -> with: 32/8 heads, 32 sequences of 40 / 100 / 200 / 400 tokens
@@ -66,8 +68,8 @@ BASS_HD inline int unit_pad(bool shared, int rows, int heads) { return is_tile(s
 // more beginning and end, and every row one more partial result.  us per layer, separate / together, prefixes of 256 / 512 / 1024 / 2048 / 4096 tokens, 200
 // of their own, 4 query tokens: 32 heads, 2 sequences 13.5 / 13.9 / 14.9 / 18.5 / 24.1 and 13.2 / 13.7 / 14.5 / 16.6 / 21.6, 4 sequences 13.8 / 16.0 / 18.6 / 23.1 / 32.8 and 13.7 /
 // 15.4 / 16.7 / 18.6 / 22.8, 8 sequences 19.2 / 23.2 / 31.4 / 49.2 / 83.2 and 16.3 / 16.5 / 18.0 / 20.1 / 25.5; 32/8 heads, 8 sequences 14.0 / 14.7 / 15.7 / 20.3 / 29.5 and 13.9 / 15.7 / 17.3 /
-// 20.4 / 24.0, 32 sequences 21.7 / 25.0 / 33.2 / 54.2 / 94.1 and 24.4 / 26.5 / 27.8 / 32.4 / 35.8; 64/8 heads, 8 sequences 14.6 / 15.5 / 17.0 / 21.7 / 31.4 and 18.8 / 21.9 / 25.9 / 27.1 /
-// 28.2, 32 sequences 24.1 / 27.8 / 36.2 / 58.7 / 98.1 and 26.1 / 27.3 / 33.6 / 37.5 / 45.1.  In entries saved per workgroup: from about 12 on, or 55 with tiles, whose
+// 20.4 / 24.2, 32 sequences 21.7 / 25.0 / 33.2 / 54.2 / 94.1 and 24.4 / 26.6 / 27.5 / 28.3 / 33.3; 64/8 heads, 8 sequences 14.6 / 15.5 / 17.0 / 21.7 / 31.4 and 18.8 / 21.9 / 25.9 / 27.1 /
+// 30.5, 32 sequences 24.1 / 27.8 / 36.2 / 58.7 / 98.1 and 26.1 / 27.3 / 31.1 / 35.7 / 44.0.  In entries saved per workgroup: from about 12 on, or 55 with tiles, whose
 // beginnings are long; but those are paid once for all prefixes of a batch.
 constexpr int kSavedRows = 12, kSavedTile = 55;
 BASS_HD inline int saved_by_sharing(int members, int tokens, int tiles, int tile_tok, int n_blk, int g, int Hkv, bool int8) {
