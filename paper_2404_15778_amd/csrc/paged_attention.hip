@@ -332,7 +332,7 @@ __device__ inline void paged_unit(const PagedParams& p, const PagedSegment& s, i
 
 // ---------------------------------------------------------------------------------------
 // Many query rows (a shared prefix): a wavefront has 32 NT rows of its own, 128 NT in all, and all four go through the blocks together.  A block
-// is fetched once for the workgroup, into registers two blocks ahead, and from there into LDS one block ahead, in the operand order
+// is fetched once for the workgroup, into registers two or four blocks ahead, and from there into LDS one block ahead, in the operand order
 // that it has in the pool (INT8: V as bf16, so that the codes are widened once and not by every wavefront).  Every wavefront reads the whole block
 // from LDS, 16 KB for 16 NT matrix instructions; with NT = 2 that is half of what LDS can deliver in their time.
 // Every token of a shared run is visible to every row: there are no masks.
@@ -554,6 +554,7 @@ __device__ inline void paged_tile(const PagedParams& p, const PagedSegment& s, i
         if (x < kSteps) read_k(x, t + 2);
       });
     } else {
+      // One tile: the scores of block t + 1 beside the probabilities of block t, then the values of block t beside the maximum of block t + 1.
 #pragma unroll
       for (int x = 0; x < kSteps; ++x) {
         score(0, x);
