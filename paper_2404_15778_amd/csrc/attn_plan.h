@@ -38,7 +38,7 @@ BASS_HD inline bool clamp_lengths(int& L, int& nq, int kmax, int Lcap) {
   if (nq > kmax) { nq = kmax; bad = true; }
   if (nq > Lcap) { nq = Lcap; bad = true; }
   if (L < 0) { L = 0; bad = true; }
-  if (L + nq > Lcap) { L = Lcap - nq; bad = true; }
+  if (L > Lcap - nq) { L = Lcap - nq; bad = true; }  // not L + nq > Lcap: that sum may not fit in 32 bits
   return bad;
 }
 
