@@ -25,8 +25,8 @@ constexpr int kBlockTokens = 32;  // tokens per cache block (one PV contraction 
 constexpr int kMaxWaves = 8192;   // upper bound of the attention work spread (sizes plans and workspaces)
 constexpr int kMaxPad = 8;        // upper bound of the virtual blocks per unit
 
-BASS_HD inline int imin(int a, int b) { return a < b ? a : b; }
-BASS_HD inline int imax(int a, int b) { return a > b ? a : b; }
+BASS_HD constexpr int imin(int a, int b) { return a < b ? a : b; }
+BASS_HD constexpr int imax(int a, int b) { return a > b ? a : b; }
 
 BASS_HD inline int num_blocks(int tokens) { return (tokens + kBlockTokens - 1) / kBlockTokens; }
 

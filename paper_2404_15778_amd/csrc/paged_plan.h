@@ -33,7 +33,13 @@ constexpr int kTileStart = 48;  // a workgroup that begins with a tile loses so 
 // are twice as large to merge, or with four times the units.
 constexpr int kHeadUnits = 240, kHeadBlocks = 8;
 BASS_HD inline int head_blocks(int units, int rows) { return units < kHeadUnits ? 0 : rows > 32 || units >= 4 * kHeadUnits ? 2 * kHeadBlocks : kHeadBlocks; }
-constexpr int kLeastEntries = 40;   // of a workgroup, as long as there are fewer workgroups than kPagedShares; at least the largest cost
+constexpr int kLeastEntries = 40;   // of a workgroup, as long as there are fewer workgroups than kPagedShares
+// The merge adds up a partial result of every workgroup between the first and the last one that have a block of a unit, so each of them has to have one: a
+// share must not be shorter than a block's entries.  At most that many: few rows, a kv head per wavefront; tiles, up to three times the plain cost (tile_cost:
+// the quotient stays below it, because per < 3 (per / 3 + 1)).
+constexpr int kCostTileMost = imax(imax(kCostTile1, kCostTile2), imax(kCostTile1Int8, kCostTile2Int8));
+static_assert(kLeastEntries >= kPagedWaves * imax(kCostRows1, kCostRows2), "a share has a block of every unit that it lies in");
+static_assert(kLeastEntries >= 3 * kCostTileMost, "a share has a block of every unit that it lies in");
 constexpr int kTileRows = 256;      // most query rows of a tile
 constexpr int kSlotRows = kTileRows;  // rows between the partial results of two workgroups (see partial_row)
 
