@@ -668,9 +668,16 @@ def bass_paged_verify_attention(desc, Q, Kpool, Vpool, tables, plan, O, lse, wor
 
 # ---- allocation helpers (plumbing; no arithmetic) ----------------------------------------------
 
+def _sized(nbytes, what):
+    """A size the library gave; it is 0 for a shape that its calls refuse, and an empty buffer would hide that."""
+    if nbytes == 0:
+        raise ValueError(f"{what}: bad shape, or one beyond the limits of include/bass.h")
+    return nbytes
+
+
 def alloc_page_pool(desc, device="cuda", fill_byte=None):
     """One pool (K or V) as a byte tensor; optionally filled with a byte pattern."""
-    t = _torch().empty(bass_page_pool_bytes(desc), dtype=_torch().uint8, device=device)
+    t = _torch().empty(_sized(bass_page_pool_bytes(desc), "alloc_page_pool"), dtype=_torch().uint8, device=device)
     if fill_byte is not None:
         t.fill_(fill_byte)
     return t
@@ -678,17 +685,17 @@ def alloc_page_pool(desc, device="cuda", fill_byte=None):
 
 def alloc_paged_plan(desc, device="cuda"):
     """A plan buffer of the attention over paged caches (bass_paged_attention_plan fills it)."""
-    return _torch().empty(bass_paged_attention_plan_bytes(desc), dtype=_torch().uint8, device=device)
+    return _torch().empty(_sized(bass_paged_attention_plan_bytes(desc), "alloc_paged_plan"), dtype=_torch().uint8, device=device)
 
 
 def alloc_paged_workspace(desc, device="cuda"):
     """Workspace of the attention over paged caches (it needs no clearing)."""
-    return _torch().empty(bass_paged_attention_workspace_bytes(desc), dtype=_torch().uint8, device=device)
+    return _torch().empty(_sized(bass_paged_attention_workspace_bytes(desc), "alloc_paged_workspace"), dtype=_torch().uint8, device=device)
 
 
 def alloc_page_tables_workspace(rows, n_pages, device="cuda"):
     """Workspace of bass_page_tables (it needs no clearing)."""
-    return _torch().empty(bass_page_tables_workspace_bytes(rows, n_pages), dtype=_torch().uint8, device=device)
+    return _torch().empty(_sized(bass_page_tables_workspace_bytes(rows, n_pages), "alloc_page_tables_workspace"), dtype=_torch().uint8, device=device)
 
 
 def alloc_kv_cache(desc, device="cuda", fill_byte=None):
