@@ -394,7 +394,10 @@ int bass_paged_gather_int8(const bass_paged_desc* desc, const void* Kpool, const
  * them together where that is quicker; the result is that of separate sequences up to rounding.  Numbers outside [0, n_prefixes) count as none (from
  * n_prefixes on with BASS_STATUS_LEN_CLAMPED).
  * bass_paged_verify_attention: one layer.  tables [B, max_pages].  Page numbers outside the pool: page 0 is read in their place
- * (BASS_STATUS_PAGE_CLAMPED).  A plan of another descriptor computes nothing (BASS_STATUS_PLAN_MISMATCH).  lse may be NULL.  kmax * (Hq / Hkv) <= 64.
+ * (BASS_STATUS_PAGE_CLAMPED).  A plan of another descriptor computes nothing (BASS_STATUS_PLAN_MISMATCH).  lse may be NULL.
+ * Limits of the attention, its plan and their sizes (else BASS_ERR_UNSUPPORTED, and sizes of 0): B <= 4096, kmax * (Hq / Hkv) <= 64, and
+ * B * Hkv * (8 * max_pages * page_tokens / 32 + 256) < 2^31 (entries of the work list, whatever the lengths; 1000 sequences
+ * of up to 65 536 tokens with 32 kv heads make a quarter of it).
  * plan and workspace: device, 16-byte aligned, of at least the bytes the queries say; contents irrelevant on entry; calls that overlap must not share
  * a workspace, and may share a plan.  Two launches.
  */

@@ -86,7 +86,7 @@ BASS_HD inline int saved_by_sharing(int members, int tokens, int tiles, int tile
 BASS_HD inline bool worth_sharing(int saved, int saved_by_all, bool tile) { return saved >= kSavedRows && saved_by_all >= (tile ? kSavedTile : kSavedRows); }
 // Every workgroup pays for a beginning, those with tiles more; in short lists that is much of their time, so that a tile's block counts for more there.
 // per: entries of a workgroup by the plain costs.
-BASS_HD inline int tile_cost(int cost, int per) { return (int)((int64_t)cost * per / imax(per - kTileStart, per / 3 + 1)) + 1; }
+BASS_HD constexpr int tile_cost(int cost, int per) { return (int)((int64_t)cost * per / imax(per - kTileStart, per / 3 + 1)) + 1; }
 
 struct PagedHeader {
   int32_t signature, n_runs, total, per, rem, used;
@@ -146,13 +146,24 @@ inline int32_t paged_signature(const bass_paged_desc* d) {
   return (int32_t)(h | 1u);  // never the zero of an empty buffer
 }
 
+// The list counts in 32 bits.  Most entries of a sequence and kv head with n blocks, by the costs above:
+//   own run           6 n + 56; a kv head per wavefront (n <= 16): a unit of 4 (6 n + 16) entries for at least two heads, 12 n + 32 <= 6 n + 128
+//   its part of a shared run of s blocks, which its own run is shorter by: the rule for sharing asks that the tiles take less than the sequences apart, so less
+//                     than 6 s, and a tile per sequence at most: 108 more; in a tile's cost in effect (tile_cost) at most 6 / 5 of that, from 480 entries per
+//                     workgroup on.  (Lists with less stay below 3 * 256 * 481 entries.)
+// Together less than 7.2 n + 236.
+constexpr int kEntriesPerBlock = 8, kEntriesPerUnit = 256;
+static_assert(kCostRows1 <= kCostRows2 && kCostRows2 <= 6 && kPadRows <= 56 && kPadHeads <= 64 && kPadTile <= 108 && 2 * kHeadBlocks <= 16, "bound of the list");
+constexpr bool tile_cost_bounded(int cost) { return 5 * tile_cost(cost, 480) <= 6 * cost; }
+static_assert(tile_cost_bounded(kCostTile1) && tile_cost_bounded(kCostTile2) && tile_cost_bounded(kCostTile1Int8) && tile_cost_bounded(kCostTile2Int8), "bound of the list");
+
 inline int check_paged_attention(const bass_paged_desc* d) {
   const int rc = check_paged(d);
   if (rc != BASS_OK) return rc;
   if (d->B > kMaxPagedBatch || (int64_t)d->kmax * (d->Hq / d->Hkv) > 64) return BASS_ERR_UNSUPPORTED;
-  // the list counts in 32 bits: every sequence's blocks, and at most as many again of shared runs
   const int64_t blocks = (int64_t)d->max_pages * (d->page_tokens / kBlockTokens);
-  if (((kCostRows2 + 3 * kCostTile2Int8 + 1) * blocks + kPadRows + kPadTile) * d->B * d->Hkv >= (1ll << 31) || 2 * (int64_t)d->B * d->kmax * d->Hq >= (1ll << 31)) return BASS_ERR_UNSUPPORTED;
+  // divided, because the product may need more than 64 bits.  Partial rows, 2 B kmax Hq <= 128 B Hkv (partial_rows), are then below 2^31 too.
+  if (kEntriesPerBlock * blocks + kEntriesPerUnit > ((1ll << 31) - 1) / ((int64_t)d->B * d->Hkv)) return BASS_ERR_UNSUPPORTED;
   return BASS_OK;
 }
 

@@ -103,3 +103,23 @@ def test_random_batches(hip, dtype, B, kmax, Hq, Hkv, prefixes, most, longest):
         seen.append(check_plan(plan, desc, ctx, nq, of, plen))
     assert max(n for n, _ in seen) >= min(prefixes, 2)  # some of them share prefixes, two at once where there are several
     assert B > 12 or min(used for _, used in seen) < SHARES  # short lists
+
+
+# sequences, slots, heads, kv heads, tokens of a page, entries of a table: the largest lists that shapes are accepted for
+@pytest.mark.parametrize("dtype", ["bf16", "int8kv"])
+@pytest.mark.parametrize("shared", [0, 1, 5])
+@pytest.mark.parametrize("B,kmax,Hq,Hkv,P,most", [(1000, 1, 32, 32, 32, 2048), (4096, 1, 8, 8, 32, 8159), (4032, 8, 256, 32, 32, 2047), (2, 16, 8, 2, 64, 33554399), (250, 7, 27, 3, 256, 44699)])
+def test_the_largest_lists(hip, dtype, shared, B, kmax, Hq, Hkv, P, most):
+    """Full tables with as many query tokens as there may be; nothing shared, one prefix of nearly everything, and five of different lengths."""
+    import paper_2404_15778_amd as bass
+    desc = bass.make_paged_desc(B, kmax, Hq, Hkv, 64, P, 100, most, dtype, 0.1)
+    assert bass.bass_paged_attention_plan_bytes(desc) > 0
+    rng = np.random.default_rng(B)
+    nq = np.full(B, kmax)
+    ctx = most * P - kmax - rng.integers(0, 200, size=B)
+    of = np.arange(B) % shared if shared else None
+    plen = most * P // np.arange(1, shared + 1) - 1000 if shared else None
+    plan, status = make_plan(hip, desc, ctx, nq, of, plen)
+    assert status == 0
+    runs, used = check_plan(plan, desc, ctx, nq, of, plen)
+    assert runs == (shared if B > 5 or shared == 1 else 0) and used == SHARES

@@ -44,3 +44,25 @@ def test_buffers_of_good_shapes():
     assert bass.alloc_page_tables_workspace(4, 50, "cpu").numel() == bass.bass_page_tables_workspace_bytes(4, 50)
     with pytest.raises(ValueError, match="alloc_page_tables_workspace"):
         bass.alloc_page_tables_workspace(0, 50, "cpu")
+
+
+# sequences, heads, kv heads, tokens of a page, entries of a table; the list has B Hkv (8 blocks + 256) entries at most
+@pytest.mark.parametrize("B,Hq,Hkv,P,most", [(1000, 32, 32, 32, 2048), (4096, 8, 8, 32, 8159), (1, 4, 4, 64, 33554399), (1, 1, 1, 32, 67108863), (64, 64, 8, 256, 65520)])
+def test_the_list_of_the_attention(B, Hq, Hkv, P, most):
+    """As documented: shapes up to the limit have sizes, and the first beyond it is refused with a size of 0."""
+    d = desc(B=B, kmax=1, Hq=Hq, Hkv=Hkv, page_tokens=P, n_pages=100)
+    entries = lambda n: B * Hkv * (8 * n * (P // 32) + 256)  # noqa: E731
+    largest = min((2 ** 31 - 1) // P, max(n for n in (((2 ** 31 - 1) // (B * Hkv) - 256) // (8 * (P // 32)) + i for i in (-1, 0, 1)) if entries(n) < 2 ** 31))
+    assert most <= largest
+    for n in (most, largest):
+        assert bass.bass_paged_attention_plan_bytes(d.replace(max_pages=n)) > 0 and bass.bass_paged_attention_workspace_bytes(d.replace(max_pages=n)) > 0
+    beyond = d.replace(max_pages=largest + 1)
+    assert bass.bass_paged_attention_plan_bytes(beyond) == 0 == bass.bass_paged_attention_workspace_bytes(beyond)
+    assert bass.lib().bass_paged_attention_plan(ctypes.byref(beyond), ONE, ONE, None, None, 0, ONE, 1 << 40, None, None) == bass.ERR_UNSUPPORTED
+
+
+def test_products_beyond_64_bits():
+    """Sizes whose products overflow are refused like any others beyond the limits."""
+    for hkv in (1 << 20, 1 << 30):
+        d = desc(B=4096, kmax=64, Hq=hkv, Hkv=hkv, page_tokens=32, n_pages=1, max_pages=(1 << 26) - 1)
+        assert bass.bass_paged_attention_plan_bytes(d) == 0 == bass.bass_paged_attention_workspace_bytes(d)
