@@ -29,6 +29,8 @@ BASS_HD constexpr int imin(int a, int b) { return a < b ? a : b; }
 BASS_HD constexpr int imax(int a, int b) { return a > b ? a : b; }
 
 BASS_HD inline int num_blocks(int tokens) { return (tokens + kBlockTokens - 1) / kBlockTokens; }
+// Pages of any size for tokens >= 0.  (A full table of pages that are no power of two may end less than a page before 2^31: nothing is added to its length.)
+BASS_HD inline int num_pages(int tokens, int page_tokens) { return tokens / page_tokens + (tokens % page_tokens != 0); }
 
 // Per-sequence lengths with the clamping the header promises.  L = cached tokens before the step,
 // nq = query tokens; on return 0 <= nq <= kmax, 0 <= L, L + nq <= Lcap.

@@ -40,7 +40,7 @@ __device__ inline int pages_needed(const PageParams& p, int r, int& bad) {
   const int most = p.max_pages * p.page_tokens;
   if (n < 0) { n = 0; bad |= BASS_STATUS_LEN_CLAMPED; }
   if (n > most) { n = most; bad |= BASS_STATUS_LEN_CLAMPED; }
-  return (n + p.page_tokens - 1) / p.page_tokens;
+  return num_pages(n, p.page_tokens);
 }
 __device__ inline int pages_held(const PageParams& p, int r) { return min(max(p.held[r], 0), p.max_pages); }
 
