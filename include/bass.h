@@ -351,7 +351,7 @@ size_t bass_page_pool_bytes(const bass_paged_desc* desc);
  * Pages that several rows hold are not copied when one of them is written: a row appends behind what it shares, and one that has to go back into it
  * gives all its pages back first (length 0) and begins again.
  * The result does not depend on the order in which anything runs.  rows, max_pages, n_pages > 0, page_tokens a multiple of 32, rows * max_pages < 2^31,
- * n_pages * page_tokens < 2^31, 0 <= kmax <= 65535.  workspace: device, 16-byte aligned, at least bass_page_tables_workspace_bytes(rows, n_pages) bytes,
+ * n_pages * page_tokens < 2^31, 0 <= kmax <= 65535, rows * kmax < 2^32, rows / 4 + n_pages / 4096 < 2^24.  workspace: device, 16-byte aligned, at least bass_page_tables_workspace_bytes(rows, n_pages) bytes,
  * contents irrelevant on entry.  One launch for few rows of a small pool, else three or four.
  */
 size_t bass_page_tables_workspace_bytes(int32_t rows, int32_t n_pages);
@@ -363,7 +363,8 @@ int bass_page_tables(int32_t rows, int32_t max_pages, int32_t page_tokens, int32
 /*
  * Keys and values of new tokens into the pages: row i of sequence b, K_new, V_new [B, kmax, Hkv, D] bf16, to slot slots[b, i]
  * (slots [B, kmax] int32; negative: the row is left out; beyond the pool: left out, BASS_STATUS_PAGE_CLAMPED).  INT8 pools: quantized as in
- * bass_kv_append.  Nothing but the rows' own bytes is written.  Two rows of one call must not have the same slot.
+ * bass_kv_append.  Nothing but the rows' own bytes is written.  Two rows of one call must not have the same slot.  Here and in the readers
+ * B * Hkv * ceil((kmax + 31) / 32) < 2^24 (workgroups of a launch), else BASS_ERR_UNSUPPORTED.
  */
 int bass_paged_append(const bass_paged_desc* desc, void* Kpool, void* Vpool, const void* K_new, const void* V_new,
                       const int32_t* slots, int32_t* dev_status, void* stream);
@@ -397,7 +398,7 @@ int bass_paged_gather_int8(const bass_paged_desc* desc, const void* Kpool, const
  * (BASS_STATUS_PAGE_CLAMPED).  A plan of another descriptor computes nothing (BASS_STATUS_PLAN_MISMATCH).  lse may be NULL.
  * Limits of the attention, its plan and their sizes (else BASS_ERR_UNSUPPORTED, and sizes of 0): B <= 4096, kmax * (Hq / Hkv) <= 64, and
  * B * Hkv * (8 * max_pages * page_tokens / 32 + 256) < 2^31 (entries of the work list, whatever the lengths; 1000 sequences
- * of up to 65 536 tokens with 32 kv heads make a quarter of it).
+ * of up to 65 536 tokens with 32 kv heads make a quarter of it), B * kmax * ceil(Hq * D / 1024) < 2^24 (workgroups of a launch).
  * plan and workspace: device, 16-byte aligned, of at least the bytes the queries say; contents irrelevant on entry; calls that overlap must not share
  * a workspace, and may share a plan.  Two launches.
  */

@@ -346,11 +346,11 @@ extern "C" int bass_page_tables(int32_t rows, int32_t max_pages, int32_t page_to
   if (page_tokens % kBlockTokens != 0 || kmax > 65535) return BASS_ERR_UNSUPPORTED;
   if ((int64_t)rows * max_pages >= (1ll << 31) || (int64_t)n_pages * page_tokens >= (1ll << 31) || (int64_t)max_pages * page_tokens >= (1ll << 31))
     return BASS_ERR_UNSUPPORTED;
-  const int64_t slot_groups = ((int64_t)rows * kmax + 255) / 256;
-  if (slot_groups > 0x7fffffff) return BASS_ERR_UNSUPPORTED;
+  const int64_t slot_groups = ((int64_t)rows * kmax + 255) / 256, row_groups = ((int64_t)rows + 3) / 4;
+  const int tiles = tiles_of(n_pages);
+  if (!grid_fits(slot_groups) || !grid_fits(tiles + row_groups)) return BASS_ERR_UNSUPPORTED;
   if (workspace_bytes < bass_page_tables_workspace_bytes(rows, n_pages)) return BASS_ERR_WORKSPACE_TOO_SMALL;
   int32_t* ws = (int32_t*)workspace;
-  const int tiles = tiles_of(n_pages);
   PageParams p{rows, max_pages, page_tokens, n_pages, kmax, tiles, length, share_from, share_len, ctx_len, n_new,
                held, tables, refs, slots, ws, ws + rows, ws + 2 * (size_t)rows, ws + 3 * (size_t)rows + 1, dev_status};
   hipStream_t s = (hipStream_t)stream;
@@ -358,10 +358,9 @@ extern "C" int bass_page_tables(int32_t rows, int32_t max_pages, int32_t page_to
     hipLaunchKernelGGL(page_tables_small, dim3(1), dim3(kSmallThreads), 0, s, p);
     return launch_status();
   }
-  const unsigned row_groups = ((unsigned)rows + 3) / 4;
-  hipLaunchKernelGGL(page_rows, dim3(row_groups), dim3(256), 0, s, p);
+  hipLaunchKernelGGL(page_rows, dim3((unsigned)row_groups), dim3(256), 0, s, p);
   hipLaunchKernelGGL(page_counts, dim3(tiles + 1), dim3(kTileThreads), 0, s, p);
-  hipLaunchKernelGGL(page_assign, dim3(tiles + row_groups), dim3(kTileThreads), 0, s, p);
+  hipLaunchKernelGGL(page_assign, dim3((unsigned)(tiles + row_groups)), dim3(kTileThreads), 0, s, p);
   if (slots && kmax > kInlineSlots) hipLaunchKernelGGL(page_slots, dim3((unsigned)slot_groups), dim3(256), 0, s, p);
   return launch_status();
 }

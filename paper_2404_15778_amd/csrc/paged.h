@@ -24,6 +24,9 @@ inline size_t page_block_bytes(const bass_paged_desc* d) {
   return d->dtype == BASS_DTYPE_INT8KV ? i8_block_bytes(d->D) : (size_t)kBlockTokens * d->D * 2;
 }
 
+// A launch counts its threads in 32 bits; larger ones are refused before anything is enqueued.
+inline bool grid_fits(int64_t groups, int threads = 256) { return groups * threads < (1ll << 32); }
+
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 #ifdef __HIPCC__

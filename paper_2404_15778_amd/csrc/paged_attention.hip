@@ -808,8 +808,8 @@ extern "C" int bass_paged_verify_attention(const bass_paged_desc* d, const void*
   hipStream_t s = (hipStream_t)stream;
   const bool int8 = d->dtype == BASS_DTYPE_INT8KV;
   const dim3 grid(kPagedShares), block(64 * kPagedWaves);
-  const int head_groups = (d->Hq + 1024 / d->D - 1) / (1024 / d->D);
-  const dim3 merge_grid((unsigned)(d->B * d->kmax * head_groups));
+  const dim3 merge_grid((unsigned)merge_groups(d));
+  const int head_groups = (int)(merge_groups(d) / ((int64_t)d->B * d->kmax));
   if (d->D == 128) {
     if (int8) hipLaunchKernelGGL((paged_attn<128, true>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((paged_attn<128, false>), grid, block, 0, s, p);

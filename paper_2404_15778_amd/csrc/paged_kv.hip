@@ -240,7 +240,7 @@ static int launch_paged_rows(const bass_paged_desc* d, bool gather, PagedRows p,
   // the blocks that kmax consecutive tokens can touch
   p.windows = (int)(((int64_t)d->kmax + kBlockTokens - 2) / kBlockTokens + 1);
   const int64_t groups = (int64_t)d->B * p.windows * d->Hkv;
-  if (groups > 0x7fffffff) return BASS_ERR_UNSUPPORTED;
+  if (!grid_fits(groups)) return BASS_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)groups), block(256);
   hipStream_t s = (hipStream_t)stream;
   const bool int8 = d->dtype == BASS_DTYPE_INT8KV;

@@ -157,6 +157,10 @@ static_assert(kCostRows1 <= kCostRows2 && kCostRows2 <= 6 && kPadRows <= 56 && k
 constexpr bool tile_cost_bounded(int cost) { return 5 * tile_cost(cost, 480) <= 6 * cost; }
 static_assert(tile_cost_bounded(kCostTile1) && tile_cost_bounded(kCostTile2) && tile_cost_bounded(kCostTile1Int8) && tile_cost_bounded(kCostTile2Int8), "bound of the list");
 
+// Workgroups of the merge: one for a query token and this many of its heads.
+constexpr int kMergeElems = 1024;
+inline int64_t merge_groups(const bass_paged_desc* d) { return (int64_t)d->B * d->kmax * ((d->Hq + (int64_t)(kMergeElems / d->D) - 1) / (kMergeElems / d->D)); }
+
 inline int check_paged_attention(const bass_paged_desc* d) {
   const int rc = check_paged(d);
   if (rc != BASS_OK) return rc;
@@ -164,6 +168,7 @@ inline int check_paged_attention(const bass_paged_desc* d) {
   const int64_t blocks = (int64_t)d->max_pages * (d->page_tokens / kBlockTokens);
   // divided, because the product may need more than 64 bits.  Partial rows, 2 B kmax Hq <= 128 B Hkv (partial_rows), are then below 2^31 too.
   if (kEntriesPerBlock * blocks + kEntriesPerUnit > ((1ll << 31) - 1) / ((int64_t)d->B * d->Hkv)) return BASS_ERR_UNSUPPORTED;
+  if (!grid_fits(merge_groups(d))) return BASS_ERR_UNSUPPORTED;
   return BASS_OK;
 }
 

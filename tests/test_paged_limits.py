@@ -66,3 +66,30 @@ def test_products_beyond_64_bits():
     for hkv in (1 << 20, 1 << 30):
         d = desc(B=4096, kmax=64, Hq=hkv, Hkv=hkv, page_tokens=32, n_pages=1, max_pages=(1 << 26) - 1)
         assert bass.bass_paged_attention_plan_bytes(d) == 0 == bass.bass_paged_attention_workspace_bytes(d)
+
+
+def test_launches_of_more_threads_than_are_counted():
+    """A launch counts its threads in 32 bits; what would need more is refused before anything is enqueued.  Just below, everything else has to be in order."""
+    L, U = bass.lib(), bass.ERR_UNSUPPORTED
+
+    def rows(append, **kw):
+        d = desc(**kw)
+        if append:
+            return L.bass_paged_append(ctypes.byref(d), ONE, ONE, ONE, ONE, ONE, None, None)
+        return L.bass_paged_gather(ctypes.byref(d), ONE, ONE, ONE, ONE, ONE, ONE, ONE, None, None)
+
+    for append in (True, False):
+        assert rows(append, B=1 << 19, kmax=2, Hq=16, Hkv=16) == U         # 2 windows of 32 tokens
+        assert rows(append, B=1 << 20, kmax=1, Hq=16, Hkv=16) == U
+        assert rows(append, B=16, kmax=(1 << 20) + 1, Hq=32, Hkv=32) == U
+
+    def tables(rows, max_pages, kmax):
+        slots = ONE if kmax else None
+        return L.bass_page_tables(rows, max_pages, 32, 50, ONE, None, None, ONE, ONE, ONE, kmax, slots, slots, slots, ONE, 1 << 40, None, None)
+
+    assert tables(1 << 26, 1, 0) == U
+    assert tables(65538, 1, 65535) == U
+    d = desc(B=4096, kmax=64, Hq=1024, Hkv=1024, D=128, page_tokens=32, n_pages=100, max_pages=1)
+    assert bass.bass_paged_attention_plan_bytes(d) == 0 == bass.bass_paged_attention_workspace_bytes(d)
+    assert L.bass_paged_verify_attention(ctypes.byref(d), *[ONE] * 6, None, ONE, 1 << 60, None, None) == U
+    assert bass.bass_paged_attention_plan_bytes(d.replace(B=4095, Hq=512, Hkv=512)) > 0
