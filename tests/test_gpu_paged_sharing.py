@@ -218,3 +218,18 @@ def test_int8_pages_and_caches_of_their_own(hip, i, D):
     assert np.abs(want_lse).max() < 24 and int(da.status.item()) == 0
     assert np.abs(lse - lsec).max() <= 2 ** -13
     assert (np.abs(O - Oc) <= (2 * 2 ** -8 + 2 ** -14) * A + 2 ** -8 * np.abs(Oc)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "int8kv"])
+@pytest.mark.parametrize("i", [None, 0, 1, 2])
+def test_pools_beyond_four_gigabytes(hip, dtype, i):
+    """All pages behind the first 2^32 bytes of a pool, in every form, apart and together."""
+    batch = one(i or 0, dtype, seed=5)
+    page = 32 * batch.Hkv * (batch.D + 4 if dtype == "int8kv" else 2 * batch.D)
+    front = 2 ** 32 // page + 1
+    batch.tables[batch.tables >= 0] += front
+    batch.n_pages += front
+    pg = batch.pages(hip)
+    assert pg.K.numel() > 2 ** 32 + 100 * page
+    batch.check(hip, pg=pg, share=i is not None)
+    assert [form(rows, tiles) for rows, tiles, _ in shared_runs(pg)] == ([] if i is None else [i])
