@@ -382,8 +382,15 @@ int bass_paged_gather_int8(const bass_paged_desc* desc, const void* Kpool, const
 
 /*
  * Verification attention over paged caches; what bass_verify_attention computes, with O [B, kmax, Hq, D] in bf16, as the output
- * projection takes it.  The step's own K/V rows have been appended (bass_paged_append).  INT8 pools: queries are quantized per row as in
- * BASS_DTYPE_INT8KV, but with inv = 127 * (1 / amax), two rounded steps, for 127 / amax: codes differ where x * 127 / amax is within a rounding of a half.
+ * projection takes it.  The step's own K/V rows have been appended (bass_paged_append).
+ * Precision: scores, maxima, sums and what is joined from several workgroups have 32 bits; every probability is rounded to bf16 (over INT8 pools times its
+ * token's scale) before it multiplies V, and O is.  An element of O is off by at most 2^-8 sum_j p_j |v_j| + 2^-8 |O|, the whole of it by 1.8e-3 to 2.4e-3
+ * (2-norms), of which the rounding of O alone is 1.7e-3.  bass_verify_attention returns 32 bits, and multiplies all 24 bits of a probability where
+ * sequences and query rows are few.  A masked element of V has probability zero in the product, so where V is infinite or NaN at one of
+ * the step's own tokens, that head element is NaN for the sequence's earlier query tokens too, as in bass_verify_attention.
+ * INT8 pools: queries are quantized per row as in BASS_DTYPE_INT8KV, but with inv = 127 * (1 / amax), two rounded steps, for 127 / amax: codes differ by one
+ * where x * 127 / amax is within a rounding of a half (one element in about 4.5 % of rows of 128, 2.3 % of rows of 64), so that such rows agree with
+ * the same rows over INT8 caches per sequence up to a step of a query's code, the others up to rounding.
  *
  * bass_paged_attention_plan: the division of a step's work over the GPU, one small launch for all layers.
  *   ctx_len, draft_len [B]    as in bass_verify_attention; ctx_len + draft_len <= max_pages * page_tokens (else clamped, BASS_STATUS_LEN_CLAMPED)

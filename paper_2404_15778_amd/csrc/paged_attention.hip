@@ -10,12 +10,18 @@
 // head of its own.  More rows: every wavefront has rows of its own, and they go through the blocks together.
 // paged_merge: joins the partial results and writes O, lse and the zeros of unused rows.
 //
+// Precision: 32 bits but for the operands of the V product and O.  Probabilities are bf16 there, one matrix instruction for each (a second and third part, as
+// the kernels for few rows of caches per sequence multiply them, would be two and three: in tiles these instructions are half of the work), and over INT8 pools
+// they are rounded behind the product with the token's scale.  Error of O against 64 bits 1.8e-3 - 2.4e-3, 1.65e-3 with 32 bits everywhere and O in bf16.
+//
 // us per layer, attention + merge.  Few rows: bound by the trips to memory of a launch, one behind the other (8 answers of up to 7 tokens to a prompt of 1500, 32 heads:
 // 14 + 4 for 37 MB), and in long contexts by memory (16 sequences of up to 8192 tokens: 21 + 4 for 88 MB, 4.2 TB/s).  Tiles: 3 prefixes of up to 8000 tokens, 32
 // sequences of 5 tokens, 64/8 heads: 42 + 7 (16 GFLOP; every workgroup has but a few blocks between the 6 us that a tile's beginning takes and the
 // 3 of its end); a prefix of 16 384, 64 sequences of 8, 32/8 heads: 160 - 180 + 11 (137 GFLOP, 0.8 PFLOP/s): issue of matrix and softmax instructions from one
 // wavefront per SIMD, at the clock that the card's power leaves.  INT8, a prefix of 4096, 24 sequences of one token, 64/8 heads: 26 + 6, the same bounds.  Tiles of up to 128
 // rows: 16 sequences of 6 behind 32 768 tokens, 32 heads: 114 + 7 (555 MB, 4.9 TB/s).
+// The same with heads of 64: answers 10 + 4, ragged 13 + 4, prompts 29 + 6, document 120 + 7, INT8 prompt 19 + 5; over INT8 pools, heads of 128: answers 15 + 4, ragged 19 + 4
+// (half the bytes: the trips are the same, and a block's conversions), prompts 45 + 8, document 190 + 10.
 #include "paged_plan.h"
 #include "wide_tiles.h"
 
@@ -93,8 +99,9 @@ __device__ inline QueryTokens<NT> query_tokens(const PagedParams& p, const Paged
 }
 
 // Operand B of the score tiles.  A lane's row is c of each tile, and its two lanes (h) have the row's 16-byte chunks in turn.  A negative softmax
-// scale is moved into the queries (exact), and so is a zero; the factor that is left is positive.  INT8: quantized per row, with 127 (1 / amax) for the
-// cached rows' 127 / amax: the codes are the same but where x 127 / amax is a half to within its roundings.
+// scale is moved into the queries (exact), and so is a zero; the factor that is left is positive.  INT8: quantized per row, with 127 (1 / amax), as the header
+// says, for the 127 / amax of cached rows and of the kernels for caches per sequence: no quicker, but what this operator's results have been since it was
+// there.  The codes are the same but where x 127 / amax is a half to within its roundings: one element in 4.5 % of rows of 128, in 2.3 % of rows of 64.
 template <int D, bool kI8, int NT>
 __device__ inline void load_paged_queries(const PagedParams& p, const PagedSegment& s, const QueryTokens<NT>& tokens, int kvh, int c, int h,
                                           WideQueries<D, kI8, NT>& q) {

@@ -18,6 +18,7 @@ constexpr int kPagedWaves = 4;      // wavefronts of a workgroup
 constexpr int kPagedShares = 256;   // workgroups of the attention launch: one per compute unit
 // An entry is 1/8 us.  Of a block: up to 32 and 64 rows (four blocks at a time, a wavefront each); tiles of 128 and 256 rows (a block at a time, all
 // wavefronts) over bf16 and INT8 pages.  Of the end of a unit, with the beginning of the next: by a wavefront per head, by all four, and of a tile.
+// All of it fitted to heads of 128; heads of 64, with half the bytes and products per block and the same beginnings, are divided by the same numbers.
 // Fitted to kernel times, us per layer before and with these: INT8, 6 sequences of 5 tokens behind 32 768, 32/8 heads 54 -> 35 (the workgroups without a tile had been given too
 // much); 16 sequences of 6 behind 8192, 32 heads 47 -> 41, over INT8 51 -> 39; 64 of 8 behind 16 384, 32/8 heads, INT8 222 -> 200; three prompts 46 -> 42.
 // The end of a tile at 76 / 108: 16 sequences of 4 behind 4096, 32/8 heads 24.7 / 21.1, 32 of 4 behind 1024, 64/8 heads 26.9 / 24.4; 32 of 4 behind 512, 32 heads, with the merge 31.3 / 34.2, 8 behind
@@ -77,6 +78,7 @@ BASS_HD inline int unit_pad(bool shared, int rows, int heads) { return is_tile(s
 // 20.4 / 24.2, 32 sequences 21.7 / 25.0 / 33.2 / 54.2 / 94.1 and 24.4 / 26.6 / 27.5 / 28.3 / 33.3; 64/8 heads, 8 sequences 14.6 / 15.5 / 17.0 / 21.7 / 31.4 and 18.8 / 21.9 / 25.9 / 27.1 /
 // 30.5, 32 sequences 24.1 / 27.8 / 36.2 / 58.7 / 98.1 and 26.1 / 27.3 / 31.1 / 35.7 / 44.0.  In entries saved per workgroup: from about 12 on, or 55 with tiles, whose
 // beginnings are long; but those are paid once for all prefixes of a batch.
+// (32 sequences, 32/8 heads, 512 tokens are just beyond that line, with 57, and 1.6 us longer together.)
 constexpr int kSavedRows = 12, kSavedTile = 55;
 BASS_HD inline int saved_by_sharing(int members, int tokens, int tiles, int tile_tok, int n_blk, int g, int Hkv, bool int8) {
   const int64_t apart = (int64_t)members * block_cost(false, tokens * g / members, 1, int8), together = (int64_t)tiles * block_cost(true, tile_tok * g, 1, int8);
