@@ -25,7 +25,7 @@ inline size_t page_block_bytes(const bass_paged_desc* d) {
 }
 
 // A launch counts its threads in 32 bits; larger ones are refused before anything is enqueued.
-inline bool grid_fits(int64_t groups, int threads = 256) { return groups * threads < (1ll << 32); }
+inline bool grid_fits(int64_t groups, int threads = 256) { return groups <= ((1ll << 32) - 1) / threads; }
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 

@@ -242,9 +242,9 @@ __global__ __launch_bounds__(256) void paged_gather(PagedRows p) {
 static int launch_paged_rows(const bass_paged_desc* d, bool gather, PagedRows p, void* stream) {
   // the blocks that kmax consecutive tokens can touch
   p.windows = (int)(((int64_t)d->kmax + kBlockTokens - 2) / kBlockTokens + 1);
-  const int64_t groups = (int64_t)d->B * p.windows * d->Hkv;
-  if (!grid_fits(groups)) return BASS_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)groups), block(256);
+  const int64_t per_sequence = (int64_t)p.windows * d->Hkv;  // by itself first: the product with B may need more than 64 bits
+  if (!grid_fits(per_sequence) || !grid_fits(d->B * per_sequence)) return BASS_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)(d->B * per_sequence)), block(256);
   hipStream_t s = (hipStream_t)stream;
   const bool int8 = d->dtype == BASS_DTYPE_INT8KV;
 #define BASS_LAUNCH(kernel)                                                            \

@@ -83,6 +83,10 @@ def test_launches_of_more_threads_than_are_counted():
         assert rows(append, B=1 << 20, kmax=1, Hq=16, Hkv=16) == U
         assert rows(append, B=16, kmax=(1 << 20) + 1, Hq=32, Hkv=32) == U
 
+        # numbers of workgroups beyond 64 bits, which come out as 0 or a few there
+        for kw in (dict(B=1 << 30, kmax=(1 << 31) - 31, Hq=1 << 30, Hkv=1 << 30), dict(B=(1 << 31) - 1, kmax=(1 << 31) - 1, Hq=1 << 26, Hkv=1 << 26)):
+            assert rows(append, page_tokens=32, n_pages=1, **kw) == U
+
     def tables(rows, max_pages, kmax):
         slots = ONE if kmax else None
         return L.bass_page_tables(rows, max_pages, 32, 50, ONE, None, None, ONE, ONE, ONE, kmax, slots, slots, slots, ONE, 1 << 40, None, None)
