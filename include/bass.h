@@ -384,7 +384,7 @@ int bass_paged_gather_int8(const bass_paged_desc* desc, const void* Kpool, const
  * Verification attention over paged caches; what bass_verify_attention computes, with O [B, kmax, Hq, D] in bf16, as the output
  * projection takes it.  The step's own K/V rows have been appended (bass_paged_append).
  * Precision: scores, maxima, sums and what is joined from several workgroups have 32 bits; every probability is rounded to bf16 (over INT8 pools times its
- * token's scale) before it multiplies V, and O is.  An element of O is off by at most 2^-8 sum_j p_j |v_j| + 2^-8 |O|, the whole of it by 1.8e-3 to 2.4e-3
+ * token's scale) before it multiplies V, and O is.  Beside what 32 bits leave, an element of O is off by at most 2^-8 sum_j p_j |v_j| + 2^-8 |O|, the whole of it by 1.8e-3 to 2.4e-3
  * (2-norms), of which the rounding of O alone is 1.7e-3.  bass_verify_attention returns 32 bits, and multiplies all 24 bits of a probability where
  * sequences and query rows are few.  A masked element of V has probability zero in the product, so where V is infinite or NaN at one of
  * the step's own tokens, that head element is NaN for the sequence's earlier query tokens too, as in bass_verify_attention.

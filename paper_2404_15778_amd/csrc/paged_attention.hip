@@ -726,6 +726,7 @@ constexpr int kMergeRound = 8;
 template <int D>
 __global__ __launch_bounds__(256) void paged_merge(PagedParams p, int head_groups) {
   constexpr int kLanes = D / 4, kRows = 256 / kLanes;
+  static_assert(kRows == kMergeElems / D, "merge_groups counts the workgroups");
   const int tok = blockIdx.x / head_groups, b = tok / p.kmax, i = tok - b * p.kmax;
   const int hq = (int)(blockIdx.x % head_groups) * kRows + threadIdx.x / kLanes, q4 = threadIdx.x % kLanes;
   const PagedHeader* header = p.header;
